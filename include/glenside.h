@@ -308,6 +308,82 @@ int glenside_program_rewrite(const char* text, const char* strategy, const int64
                              const gs_named_ap* tensors, int n_tensors, const gs_named_int* ints,
                              int n_ints, char* out_text, size_t out_capacity, size_t* out_needed);
 
+/* ---------------------------------------------------------------------------------------------
+ * EXT: microscaled 4-bit floats (MX4).  Every access element -- its compute dimensions flattened to
+ * K numbers -- is held as B = ceil(K / 32) blocks of 32 four-bit floats that share a scale:
+ *   values: ((S_A), (B, 16 bytes)); number 2 i of a block in the low half of byte i, 2 i + 1 in the
+ *           high half, as OCP e2m1 (sign, 2 bits of exponent, 1 of mantissa: 0 0.5 1 1.5 2 3 4 6);
+ *           codes behind K are zero;
+ *   scales: ((S_A), (B up to a multiple of 8)) bytes, OCP e8m0: 2^(byte - 127), 255 = NaN; bytes
+ *           behind B are zero.
+ * A number is its e2m1 value times its block's scale; a NaN scale makes a block's 32 numbers NaN.    */
+typedef struct {
+  void* values;               /* device pointer, 16-byte aligned, caller-owned               */
+  void* scales;               /* device pointer, 16-byte aligned, caller-owned               */
+  int32_t rank;               /* |S_A| + |S_C|, at most GS_MAX_RANK                          */
+  int32_t n_access;           /* |S_A|                                                       */
+  int64_t shape[GS_MAX_RANK]; /* S_A ++ S_C, in numbers                                      */
+} gs_mx4;
+
+/* Bytes of the two arrays of a pattern of m's shape; non-zero status if that is impossible.  Host only. */
+int glenside_mx4_sizes(const gs_mx4* m, size_t* values_bytes, size_t* scales_bytes);
+/* in (bf16 or f32) -> out of its shape and split.  A block's scale is 2^(floor(log2 max|x|) - 2), at
+ * least 2^-127 (also where all are zero); numbers are divided by it and rounded to the nearest e2m1 value,
+ * ties to the even code, magnitudes above 6 to 6; signs of zeros are kept.  A block with an infinity or
+ * a NaN becomes NaN.                                                                             */
+int glenside_mx4_quantize(const gs_ap* in, gs_mx4* out, void* stream);
+/* The numbers as bf16 or f32 (exact; beyond the type's range infinite).                          */
+int glenside_mx4_dequantize(const gs_mx4* in, gs_ap* out, void* stream);
+/* compute dotProd (cartProd a0 a1) as glenside_cartesian_dot has it, on MX4 operands; products are exact, sums are
+ * in fp32.  out ((m.., n..),()) of bf16 or f32, act as there.  A compute shape without elements gives zeros.
+ * workspace: glenside_mx4_dot_workspace bytes (may be 0; 16-byte aligned).                         */
+int glenside_mx4_dot(const gs_mx4* a0, const gs_mx4* a1, gs_ap* out, int act, void* workspace,
+                     size_t workspace_bytes, void* stream);
+size_t glenside_mx4_dot_workspace(const gs_mx4* a0, const gs_mx4* a1);
+/* The same with a0 in bf16, as it is: products of activations with MX4 weights.                   */
+int glenside_mx4_weight_dot(const gs_ap* a0, const gs_mx4* a1, gs_ap* out, int act, void* workspace,
+                            size_t workspace_bytes, void* stream);
+size_t glenside_mx4_weight_dot_workspace(const gs_ap* a0, const gs_mx4* a1);
+
+/* A cache of keys and values in pages of page_size tokens (a multiple of 16, up to 4096), `heads` heads of head_dim
+ * numbers (64, 96, 128, 192 or 256) each.  data: ((n_pages, heads), (block)), a block's bytes being, with P tokens of D
+ * numbers in blocks of 32 as above,
+ *   keys ((P),(D/2 bytes)), values ((P/4),(D/8),(4 tokens),(4 bytes)), scales of keys ((P),(D/32)) and of
+ *   values ((P/4),(D/32),(4 tokens)): 4 tokens' pieces of 8 numbers lie together, the order in which
+ *   attention sums them.
+ * A sequence is a row of `table` (i32 ((batch),(W))): token t lies in page table[b][t / P] at t % P.  Entries that are
+ * no page (below 0 or n_pages and above) are allowed where tokens are missing.                       */
+typedef struct {
+  void* data;                 /* device pointer, 16-byte aligned, caller-owned               */
+  int64_t n_pages;
+  int32_t page_size, heads, head_dim;
+  int32_t reserved;           /* must be 0                                                   */
+} gs_mx4_cache;
+/* Bytes of a cache's data; 0 if the description is impossible.  Host only.                       */
+size_t glenside_mx4_cache_bytes(const gs_mx4_cache* cache);
+/* Tokens first[b] .. first[b] + T - 1 of every sequence := keys k[b], values v[b], quantised as by
+ * glenside_mx4_quantize.  k, v ((batch, T, heads),(head_dim)), both bf16 or both f32; first, counts i32
+ * ((batch),()); counts (NULL: T everywhere) says how many of the T are tokens.  Tokens at positions
+ * below 0 or W P and above, or in entries that are no page, are dropped.  Two tokens in one place race. */
+int glenside_mx4_cache_append(const gs_mx4_cache* cache, const gs_ap* table, const gs_ap* first, const gs_ap* counts,
+                              const gs_ap* k, const gs_ap* v, void* stream);
+/* The same tokens read back into k, v (bf16 or f32); zeros where a token would have been dropped.   */
+int glenside_mx4_cache_read(const gs_mx4_cache* cache, const gs_ap* table, const gs_ap* first, gs_ap* k, gs_ap* v,
+                            void* stream);
+/* Attention of Lq queries of every sequence over its cached tokens 0 .. lengths[b] - 1, the queries being its last:
+ * query i is at position p = lengths[b] - Lq + i and sees the tokens t <= p with p - t < window or t < sinks
+ * (window 0: all t <= p), except tokens in entries that are no page.
+ *   out[b,i,h] = sum_t softmax_t(scale q[b,i,h] . k[b,t,h / G]) v[b,t,h / G],   G = query heads / cache heads.
+ * A query that sees nothing, or whose scores are all -infinity, gives zeros; tokens that a query does not see
+ * have no part in its result, whatever they hold.  Scores, weights and sums are fp32, weights are rounded to bf16
+ * for their product with the values.  q ((batch, Lq, G heads),(head_dim)) bf16; out of its shape and split, bf16 or f32;
+ * lengths i32 ((batch),()), taken as at least 0 and at most W P.
+ * workspace: glenside_mx4_attend_workspace bytes (may be 0; 16-byte aligned).                       */
+int glenside_mx4_attend(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table, const gs_ap* lengths,
+                        float scale, int64_t window, int64_t sinks, gs_ap* out, void* workspace,
+                        size_t workspace_bytes, void* stream);
+size_t glenside_mx4_attend_workspace(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -39,6 +39,9 @@ EXPORTS = (
     "glenside_conv2d_direct_static", "glenside_conv2d_direct_static_limit",
     "glenside_program_shape", "glenside_program_eval", "glenside_program_workspace",
     "glenside_program_rewrite", "glenside_depthwise_conv2d", "glenside_conv2d_direct_packed_with_projection",
+    "glenside_mx4_sizes", "glenside_mx4_quantize", "glenside_mx4_dequantize", "glenside_mx4_dot", "glenside_mx4_dot_workspace",
+    "glenside_mx4_weight_dot", "glenside_mx4_weight_dot_workspace", "glenside_mx4_cache_bytes", "glenside_mx4_cache_append",
+    "glenside_mx4_cache_read", "glenside_mx4_attend", "glenside_mx4_attend_workspace",
 )
 
 
@@ -46,6 +49,16 @@ class gs_ap(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("rank", ctypes.c_int32),
                 ("n_access", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("shape", ctypes.c_int64 * GS_MAX_RANK)]
+
+
+class gs_mx4(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rank", ctypes.c_int32), ("n_access", ctypes.c_int32),
+                ("shape", ctypes.c_int64 * GS_MAX_RANK)]
+
+
+class gs_mx4_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class gs_named_ap(ctypes.Structure):
@@ -112,6 +125,22 @@ def lib() -> ctypes.CDLL:
         L.glenside_pair.argtypes = [ap_p, ap_p, ap_p, vp]
         L.glenside_cartesian_dot_blocked.argtypes = [ap_p, ap_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ap_p, vp]
         L.glenside_depthwise_conv2d.argtypes = [ap_p, ap_p, i64_p, i64_p, ctypes.c_int, ap_p, vp]
+        mx_p, cache_p, size_p, size = ctypes.POINTER(gs_mx4), ctypes.POINTER(gs_mx4_cache), ctypes.POINTER(ctypes.c_size_t), ctypes.c_size_t
+        L.glenside_mx4_sizes.argtypes = [mx_p, size_p, size_p]
+        L.glenside_mx4_quantize.argtypes = [ap_p, mx_p, vp]
+        L.glenside_mx4_dequantize.argtypes = [mx_p, ap_p, vp]
+        L.glenside_mx4_dot.argtypes = [mx_p, mx_p, ap_p, ctypes.c_int, vp, size, vp]
+        L.glenside_mx4_dot_workspace.argtypes = [mx_p, mx_p]
+        L.glenside_mx4_weight_dot.argtypes = [ap_p, mx_p, ap_p, ctypes.c_int, vp, size, vp]
+        L.glenside_mx4_weight_dot_workspace.argtypes = [ap_p, mx_p]
+        L.glenside_mx4_cache_bytes.argtypes = [cache_p]
+        L.glenside_mx4_cache_append.argtypes = [cache_p, ap_p, ap_p, ap_p, ap_p, ap_p, vp]
+        L.glenside_mx4_cache_read.argtypes = [cache_p, ap_p, ap_p, ap_p, ap_p, vp]
+        L.glenside_mx4_attend.argtypes = [ap_p, cache_p, ap_p, ap_p, ctypes.c_float, ctypes.c_int64, ctypes.c_int64, ap_p, vp, size, vp]
+        L.glenside_mx4_attend_workspace.argtypes = [ap_p, cache_p, ap_p]
+        for f in (L.glenside_mx4_dot_workspace, L.glenside_mx4_weight_dot_workspace, L.glenside_mx4_cache_bytes,
+                  L.glenside_mx4_attend_workspace):
+            f.restype = size
         _bind_native(L)
         _lib = L
     return _lib
@@ -429,3 +458,80 @@ def program_rewrite(text: str, strategy: str, tensors, ints=None, params: Sequen
     _check(L.glenside_program_rewrite(text.encode(), strategy.encode(), _i64(params) if params else None,
                                       len(params), ta, nt, ia, ni, buf, need.value, None), "program_rewrite")
     return buf.value.decode()
+
+
+# ---------------------------------------------------------------------------------------------
+# microscaled 4-bit floats (MX4): blocks of 32 e2m1 numbers with an e8m0 scale
+# ---------------------------------------------------------------------------------------------
+
+
+class Mx4(NamedTuple):
+    """An access pattern held in MX4: `values` S_A ++ (blocks, 16 bytes), `scales` S_A ++ (blocks up to a multiple of 8),
+    both of one byte per element (uint8, or torch's own names for the formats); the numbers' shape S_A ++ S_C and |S_A|."""
+    values: torch.Tensor
+    scales: torch.Tensor
+    shape: Tuple[int, ...]
+    n_access: int
+
+
+class Mx4Cache(NamedTuple):
+    """Pages of keys and values held in MX4: `data` (pages, heads, bytes of a block), see `mx4_cache`."""
+    data: torch.Tensor
+    page_size: int
+    head_dim: int
+
+
+def mx4_quantize(x: torch.Tensor, n_access: Optional[int] = None, out: Optional[Mx4] = None) -> Mx4:
+    """The numbers of (access x n_access), bfloat16 or float32, in MX4; n_access is the last dimension by default."""
+    n = x.dim() - 1 if n_access is None else n_access
+    pair = _m().mx4_quantize(x, n, out)
+    return out if out is not None else Mx4(pair[0], pair[1], tuple(x.shape), n)
+
+
+def mx4_dequantize(m: Mx4, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The numbers as bfloat16 (default) or float32."""
+    return _m().mx4_dequantize(m, out_dtype, out)
+
+
+def mx4_dot(a0: Mx4, a1: Mx4, out_dtype: Optional[torch.dtype] = None, act: int = GS_ACT_NONE,
+            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """compute dotProd (cartProd a0 a1) of two MX4 patterns -> float32 (default) or bfloat16 of shape S_A(a0) ++ S_A(a1)."""
+    return _m().mx4_dot(a0, a1, out_dtype, act, out, workspace)
+
+
+def mx4_weight_dot(x: torch.Tensor, w: Mx4, n_access: Optional[int] = None, out_dtype: Optional[torch.dtype] = None,
+                   act: int = GS_ACT_NONE, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """compute dotProd (cartProd (access x n_access) w) of bfloat16 x with MX4 weights, x not rounded any further."""
+    return _m().mx4_weight_dot(x, w, x.dim() - 1 if n_access is None else n_access, out_dtype, act, out, workspace)
+
+
+def mx4_cache(n_pages: int, heads: int, page_size: int, head_dim: int, device) -> Mx4Cache:
+    """A new cache, every number zero."""
+    d = gs_mx4_cache()
+    d.n_pages, d.heads, d.page_size, d.head_dim = n_pages, heads, page_size, head_dim
+    need = int(lib().glenside_mx4_cache_bytes(ctypes.byref(d)))
+    if need == 0:
+        raise GlensideError(GS_ERR_UNSUPPORTED, "mx4_cache")
+    return Mx4Cache(torch.zeros((n_pages, heads, need // (n_pages * heads)), dtype=torch.uint8, device=device), page_size, head_dim)
+
+
+def mx4_cache_append(cache: Mx4Cache, table: torch.Tensor, first: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     counts: Optional[torch.Tensor] = None) -> None:
+    """Tokens first[b] .. of every sequence := k, v (batch, T, heads, head_dim); the first counts[b] of them where given."""
+    _m().mx4_cache_append(cache, table, first, counts, k, v)
+
+
+def mx4_cache_read(cache: Mx4Cache, table: torch.Tensor, first: torch.Tensor, n_tokens: int,
+                   out_dtype: Optional[torch.dtype] = None, k: Optional[torch.Tensor] = None,
+                   v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens first[b] .. first[b] + n_tokens - 1 of every sequence as bfloat16 (default) or float32."""
+    return _m().mx4_cache_read(cache, table, first, n_tokens, out_dtype, k, v)
+
+
+def mx4_attend(q: torch.Tensor, cache: Mx4Cache, table: torch.Tensor, lengths: torch.Tensor, scale: float, window: int = 0,
+               sinks: int = 0, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the last queries q (batch, Lq, heads, head_dim) of every sequence over its lengths[b] cached tokens,
+    causal, over a sliding window with the first `sinks` tokens kept where `window` is not zero."""
+    return _m().mx4_attend(q, cache, table, lengths, scale, window, sinks, out_dtype, out, workspace)

@@ -10,17 +10,7 @@
 
 using namespace gs;
 
-namespace {
-
-int64_t prod(const int64_t* v, int n) {
-  int64_t p = 1;
-  for (int i = 0; i < n; ++i) p *= v[i];
-  return p;
-}
-
-int64_t numel(const gs_ap* a) { return prod(a->shape, a->rank); }
-int64_t access_numel(const gs_ap* a) { return prod(a->shape, a->n_access); }
-int64_t compute_numel(const gs_ap* a) { return prod(a->shape + a->n_access, a->rank - a->n_access); }
+namespace gs {
 
 // Structural check of one access pattern.  `need_data` = the kernels will dereference it.
 int check_ap(const gs_ap* a, bool need_data) {
@@ -41,6 +31,26 @@ int check_ap(const gs_ap* a, bool need_data) {
   }
   return GS_OK;
 }
+
+int launch_status(hipError_t e) {
+  if (e == hipSuccess) return GS_OK;
+  if (e == hipErrorInvalidValue) return GS_ERR_UNSUPPORTED;
+  return GS_ERR_LAUNCH;
+}
+
+}  // namespace gs
+
+namespace {
+
+int64_t prod(const int64_t* v, int n) {
+  int64_t p = 1;
+  for (int i = 0; i < n; ++i) p *= v[i];
+  return p;
+}
+
+int64_t numel(const gs_ap* a) { return prod(a->shape, a->rank); }
+int64_t access_numel(const gs_ap* a) { return prod(a->shape, a->n_access); }
+int64_t compute_numel(const gs_ap* a) { return prod(a->shape + a->n_access, a->rank - a->n_access); }
 
 bool same_shape(const gs_ap* a, const gs_ap* b) {
   if (a->rank != b->rank) return false;
@@ -65,12 +75,6 @@ uint32_t lowest_bits(int dtype) {
     case GS_F8: return 0xfeu;           // -448: e4m3 has no infinity
     default: return 0xff800000u;        // -inf
   }
-}
-
-int launch_status(hipError_t e) {
-  if (e == hipSuccess) return GS_OK;
-  if (e == hipErrorInvalidValue) return GS_ERR_UNSUPPORTED;
-  return GS_ERR_LAUNCH;
 }
 
 // Shape rule of `windows` with optional padding.  Fills dims of the result.

@@ -12,6 +12,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -36,6 +37,18 @@ struct Api {
   decltype(&glenside_program_shape) program_shape;
   decltype(&glenside_program_workspace) program_workspace;
   decltype(&glenside_program_eval) program_eval;
+  decltype(&glenside_mx4_sizes) mx4_sizes;
+  decltype(&glenside_mx4_quantize) mx4_quantize;
+  decltype(&glenside_mx4_dequantize) mx4_dequantize;
+  decltype(&glenside_mx4_dot) mx4_dot;
+  decltype(&glenside_mx4_dot_workspace) mx4_dot_workspace;
+  decltype(&glenside_mx4_weight_dot) mx4_weight_dot;
+  decltype(&glenside_mx4_weight_dot_workspace) mx4_weight_dot_workspace;
+  decltype(&glenside_mx4_cache_bytes) mx4_cache_bytes;
+  decltype(&glenside_mx4_cache_append) mx4_cache_append;
+  decltype(&glenside_mx4_cache_read) mx4_cache_read;
+  decltype(&glenside_mx4_attend) mx4_attend;
+  decltype(&glenside_mx4_attend_workspace) mx4_attend_workspace;
 } api;
 PyObject* error_class;
 
@@ -513,6 +526,238 @@ PyObject* py_program_eval(PyObject*, PyObject* const* p, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------
+// microscaled 4-bit floats
+// ---------------------------------------------------------------------------------------------
+
+// Storage of one byte per element, dense.
+void* bytes_of(const at::Tensor& t) {
+  if (t.element_size() != 1 || !t.is_contiguous()) {
+    PyErr_SetString(PyExc_ValueError, "4-bit numbers, their scales and caches are dense tensors of bytes");
+    throw Failed{};
+  }
+  return t.data_ptr();
+}
+
+// All operands of a call lie on one device.
+void same_device(const at::Tensor& a, std::initializer_list<const at::Tensor*> others) {
+  for (const at::Tensor* t : others)
+    if (t->defined() && t->device() != a.device()) {
+      PyErr_SetString(PyExc_ValueError, "the tensors of a call are on one device");
+      throw Failed{};
+    }
+}
+
+PyObject* item(PyObject* tuple, Py_ssize_t i, Py_ssize_t size, const char* what) {
+  if (!PyTuple_Check(tuple) || PyTuple_GET_SIZE(tuple) != size) {
+    PyErr_Format(PyExc_TypeError, "%s is wanted", what);
+    throw Failed{};
+  }
+  return PyTuple_GET_ITEM(tuple, i);
+}
+
+// binding.Mx4: (values, scales, shape, n_access)
+struct Mx4 {
+  at::Tensor values, scales;
+  gs_mx4 d{};
+  explicit Mx4(PyObject* o) : values(tensor(item(o, 0, 4, "an Mx4"))), scales(tensor(item(o, 1, 4, "an Mx4"))) {
+    d.values = bytes_of(values);
+    d.scales = bytes_of(scales);
+    const Ints shape(item(o, 2, 4, "an Mx4"));
+    pattern(shape.v, shape.n, integer(item(o, 3, 4, "an Mx4")));
+    size_t need_values = 0, need_scales = 0;
+    call("mx4_sizes", [&] { return api.mx4_sizes(&d, &need_values, &need_scales); });
+    if (size_t(values.numel()) < need_values || size_t(scales.numel()) < need_scales) refuse(GS_ERR_SHAPE, "Mx4");
+    same_device(values, {&scales});
+  }
+  // New storage for a pattern.
+  Mx4(const int64_t* shape, int64_t rank, int64_t n_access, const at::Tensor& like) {
+    pattern(shape, rank, n_access);
+    size_t need_values = 0, need_scales = 0;
+    call("mx4_sizes", [&] { return api.mx4_sizes(&d, &need_values, &need_scales); });
+    int64_t rows = 1, v[GS_MAX_RANK + 2];
+    for (int64_t i = 0; i < n_access; ++i) rows *= v[i] = shape[i];
+    const auto bytes = at::TensorOptions().dtype(at::kByte).device(like.device());
+    const int64_t pitch = rows ? int64_t(need_scales) / rows : 0, blocks = rows ? int64_t(need_values) / rows / 16 : 0;
+    v[n_access] = pitch;
+    scales = at::empty(at::IntArrayRef(v, size_t(n_access) + 1), bytes);
+    v[n_access] = blocks;
+    v[n_access + 1] = 16;
+    values = at::empty(at::IntArrayRef(v, size_t(n_access) + 2), bytes);
+    d.values = values.data_ptr();
+    d.scales = scales.data_ptr();
+  }
+
+ private:
+  void pattern(const int64_t* shape, int64_t rank, int64_t n_access) {
+    if (rank > GS_MAX_RANK) {
+      PyErr_SetString(PyExc_ValueError, "rank above GS_MAX_RANK");
+      throw Failed{};
+    }
+    if (n_access < 0 || n_access > rank) refuse(GS_ERR_RANK, "Mx4");
+    d.rank = int32_t(rank);
+    d.n_access = int32_t(n_access);
+    for (int64_t i = 0; i < rank; ++i) d.shape[i] = shape[i];
+  }
+};
+
+// binding.Mx4Cache: (data, page_size, head_dim), data (pages, heads, bytes of a block)
+struct Cache {
+  at::Tensor data;
+  gs_mx4_cache d{};
+  explicit Cache(PyObject* o) : data(tensor(item(o, 0, 3, "an Mx4Cache"))) {
+    d.data = bytes_of(data);
+    const int64_t page = integer(item(o, 1, 3, "an Mx4Cache")), dim = integer(item(o, 2, 3, "an Mx4Cache"));
+    if (data.dim() != 3 || data.size(1) > INT32_MAX || page < 0 || page > INT32_MAX || dim < 0 || dim > INT32_MAX) refuse(GS_ERR_SHAPE, "Mx4Cache");
+    d.n_pages = data.size(0);
+    d.heads = int32_t(data.size(1));
+    d.page_size = int32_t(page);
+    d.head_dim = int32_t(dim);
+    // (where the description is impossible, the entry point says why)
+    const size_t need = api.mx4_cache_bytes(&d);
+    if (need && size_t(data.numel()) != need) refuse(GS_ERR_SHAPE, "Mx4Cache");
+  }
+};
+
+at::Tensor workspace_for(PyObject* given, size_t need, const at::Tensor& like) {
+  if (given != Py_None) {
+    const at::Tensor ws = tensor(given);
+    bytes_of(ws);
+    return ws;
+  }
+  return need ? at::empty({int64_t(need)}, at::TensorOptions().dtype(at::kByte).device(like.device())) : at::Tensor();
+}
+
+// mx4_quantize(x, n_access, out) -> (values, scales); out: an Mx4 or None
+PyObject* py_mx4_quantize(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 3, [&](PyObject*& r) {
+    const at::Tensor& x = tensor(p[0]);
+    const gs_ap xa = describe(x, integer(p[1]));
+    Mx4 out = p[2] == Py_None ? Mx4(xa.shape, xa.rank, xa.n_access, x) : Mx4(p[2]);
+    same_device(x, {&out.values});
+    void* s = stream_of(x);
+    call("mx4_quantize", [&] { return api.mx4_quantize(&xa, &out.d, s); });
+    const Owned values(THPVariable_Wrap(out.values)), scales(THPVariable_Wrap(out.scales));
+    r = PyTuple_Pack(2, values.object, scales.object);
+    if (!r) throw Failed{};
+  });
+}
+
+// mx4_dequantize(m, out_dtype, out)
+PyObject* py_mx4_dequantize(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 3, [&](PyObject*& r) {
+    const Mx4 m(p[0]);
+    Result out(p[2], p[1], at::kBFloat16, m.d.shape, m.d.rank, m.values);
+    r = out.object;
+    gs_ap oa = describe(out.value, m.d.n_access);
+    same_device(m.values, {&out.value});
+    void* s = stream_of(m.values);
+    call("mx4_dequantize", [&] { return api.mx4_dequantize(&m.d, &oa, s); });
+  });
+}
+
+// mx4_dot(a0, a1, out_dtype, act, out, workspace)
+PyObject* py_mx4_dot(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 6, [&](PyObject*& r) {
+    const Mx4 a0(p[0]), a1(p[1]);
+    const int act = code(p[3]);
+    int64_t shape[2 * GS_MAX_RANK];
+    int rank = 0;
+    for (int i = 0; i < a0.d.n_access; ++i) shape[rank++] = a0.d.shape[i];
+    for (int i = 0; i < a1.d.n_access; ++i) shape[rank++] = a1.d.shape[i];
+    Result out(p[4], p[2], at::kFloat, shape, rank, a0.values);
+    r = out.object;
+    gs_ap oa = describe_all(out.value);
+    const at::Tensor ws = workspace_for(p[5], api.mx4_dot_workspace(&a0.d, &a1.d), a0.values);
+    same_device(a0.values, {&a1.values, &out.value, &ws});
+    void *s = stream_of(a0.values), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("mx4_dot", [&] { return api.mx4_dot(&a0.d, &a1.d, &oa, act, w, bytes, s); });
+  });
+}
+
+// mx4_weight_dot(x, w, n_access, out_dtype, act, out, workspace)
+PyObject* py_mx4_weight_dot(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 7, [&](PyObject*& r) {
+    const at::Tensor& x = tensor(p[0]);
+    const Mx4 a1(p[1]);
+    const gs_ap xa = describe(x, integer(p[2]));
+    const int act = code(p[4]);
+    int64_t shape[2 * GS_MAX_RANK];
+    int rank = 0;
+    for (int i = 0; i < xa.n_access && i < xa.rank; ++i) shape[rank++] = xa.shape[i];
+    for (int i = 0; i < a1.d.n_access; ++i) shape[rank++] = a1.d.shape[i];
+    Result out(p[5], p[3], at::kFloat, shape, rank, x);
+    r = out.object;
+    gs_ap oa = describe_all(out.value);
+    const at::Tensor ws = workspace_for(p[6], api.mx4_weight_dot_workspace(&xa, &a1.d), x);
+    same_device(x, {&a1.values, &out.value, &ws});
+    void *s = stream_of(x), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("mx4_weight_dot", [&] { return api.mx4_weight_dot(&xa, &a1.d, &oa, act, w, bytes, s); });
+  });
+}
+
+// mx4_cache_append(cache, table, first, counts, k, v)
+PyObject* py_mx4_cache_append(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 6, [&](PyObject*& r) {
+    const Cache cache(p[0]);
+    const at::Tensor &table = tensor(p[1]), &first = tensor(p[2]), &k = tensor(p[4]), &v = tensor(p[5]);
+    const at::Tensor counts = p[3] == Py_None ? at::Tensor() : tensor(p[3]);
+    same_device(cache.data, {&table, &first, &counts, &k, &v});
+    const gs_ap ta = describe(table, 1), fa = describe(first, 1), ka = describe(k, 3), va = describe(v, 3);
+    gs_ap ca{};
+    if (counts.defined()) ca = describe(counts, 1);
+    void* s = stream_of(cache.data);
+    call("mx4_cache_append", [&] { return api.mx4_cache_append(&cache.d, &ta, &fa, counts.defined() ? &ca : nullptr, &ka, &va, s); });
+    Py_INCREF(Py_None);
+    r = Py_None;
+  });
+}
+
+// mx4_cache_read(cache, table, first, n_tokens, out_dtype, k, v) -> (k, v)
+PyObject* py_mx4_cache_read(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 7, [&](PyObject*& r) {
+    const Cache cache(p[0]);
+    const at::Tensor &table = tensor(p[1]), &first = tensor(p[2]);
+    const int64_t tokens = integer(p[3]);
+    if (tokens < 0 || table.dim() < 1) refuse(GS_ERR_SHAPE, "mx4_cache_read");
+    const int64_t shape[4] = {table.size(0), tokens, cache.d.heads, cache.d.head_dim};
+    const Result k(p[5], p[4], at::kBFloat16, shape, 4, cache.data);
+    const Owned k_held(k.object);
+    const Result v(p[6], p[4], at::kBFloat16, shape, 4, cache.data);
+    const Owned v_held(v.object);
+    same_device(cache.data, {&table, &first, &k.value, &v.value});
+    const gs_ap ta = describe(table, 1), fa = describe(first, 1);
+    gs_ap ka = describe(k.value, 3), va = describe(v.value, 3);
+    if (k.value.dim() > 1 && k.value.size(1) != tokens) refuse(GS_ERR_SHAPE, "mx4_cache_read");
+    void* s = stream_of(cache.data);
+    call("mx4_cache_read", [&] { return api.mx4_cache_read(&cache.d, &ta, &fa, &ka, &va, s); });
+    r = PyTuple_Pack(2, k.object, v.object);
+    if (!r) throw Failed{};
+  });
+}
+
+// mx4_attend(q, cache, table, lengths, scale, window, sinks, out_dtype, out, workspace)
+PyObject* py_mx4_attend(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 10, [&](PyObject*& r) {
+    const at::Tensor &q = tensor(p[0]), &table = tensor(p[2]), &lengths = tensor(p[3]);
+    const Cache cache(p[1]);
+    const double scale = PyFloat_AsDouble(p[4]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Failed{};
+    const int64_t window = integer(p[5]), sinks = integer(p[6]);
+    const gs_ap qa = describe(q, 3), ta = describe(table, 1), la = describe(lengths, 1);
+    Result out(p[8], p[7], at::kBFloat16, qa.shape, qa.rank, q);
+    r = out.object;
+    gs_ap oa = describe(out.value, 3);
+    const at::Tensor ws = workspace_for(p[9], p[9] == Py_None ? api.mx4_attend_workspace(&qa, &cache.d, &ta) : 0, q);
+    same_device(q, {&cache.data, &table, &lengths, &out.value, &ws});
+    void *s = stream_of(q), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("mx4_attend", [&] { return api.mx4_attend(&qa, &cache.d, &ta, &la, float(scale), window, sinks, &oa, w, bytes, s); });
+  });
+}
+
 // bind(addresses by entry point name, GlensideError)
 PyObject* py_bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded(n, 2, [&](PyObject*& r) {
@@ -545,6 +790,18 @@ PyObject* py_bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
     get("glenside_program_shape", api.program_shape);
     get("glenside_program_workspace", api.program_workspace);
     get("glenside_program_eval", api.program_eval);
+    get("glenside_mx4_sizes", api.mx4_sizes);
+    get("glenside_mx4_quantize", api.mx4_quantize);
+    get("glenside_mx4_dequantize", api.mx4_dequantize);
+    get("glenside_mx4_dot", api.mx4_dot);
+    get("glenside_mx4_dot_workspace", api.mx4_dot_workspace);
+    get("glenside_mx4_weight_dot", api.mx4_weight_dot);
+    get("glenside_mx4_weight_dot_workspace", api.mx4_weight_dot_workspace);
+    get("glenside_mx4_cache_bytes", api.mx4_cache_bytes);
+    get("glenside_mx4_cache_append", api.mx4_cache_append);
+    get("glenside_mx4_cache_read", api.mx4_cache_read);
+    get("glenside_mx4_attend", api.mx4_attend);
+    get("glenside_mx4_attend_workspace", api.mx4_attend_workspace);
     Py_INCREF(p[1]);
     Py_XDECREF(error_class);
     error_class = p[1];
@@ -559,6 +816,9 @@ PyMethodDef methods[] = {
     GS_FN("windows_reduce", py_windows_reduce), GS_FN("access_windows", py_access_windows),
     GS_FN("depthwise_conv2d", py_depthwise), GS_FN("pair_reduce", py_pair_reduce), GS_FN("transpose", py_transpose),
     GS_FN("program_eval", py_program_eval),
+    GS_FN("mx4_quantize", py_mx4_quantize), GS_FN("mx4_dequantize", py_mx4_dequantize), GS_FN("mx4_dot", py_mx4_dot),
+    GS_FN("mx4_weight_dot", py_mx4_weight_dot), GS_FN("mx4_cache_append", py_mx4_cache_append),
+    GS_FN("mx4_cache_read", py_mx4_cache_read), GS_FN("mx4_attend", py_mx4_attend),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,567 @@
+// Attention over a paged cache of microscaled 4-bit keys and values.
+//
+// A workgroup has 16 QT rows -- queries and heads that share the keys and values of one cache head -- and a part of
+// the sequence; its four waves take tiles of 64 tokens in turn, each with a running maximum and sum, and are
+// joined at the end; parts are joined by a second kernel.  Nothing passes through LDS on the way in: the cache's
+// order is the one that the matrix unit wants.  With r = lane % 16, g = lane / 16:
+//   scores: 16 tokens x 16 rows per product (16x16x32 bfloat16).  Lane (r, g) reads numbers g D/4 .. of the key of
+//     token r of a run of 16, converts them to bfloat16 (exactly: e2m1 times a power of two) and multiplies them by the same
+//     numbers of query row r.  It receives the scores of row r with tokens 4 g .. 4 g + 3 of the run.
+//   output: rows are pieces of 8 numbers of the values, columns the 16 query rows, and the sum runs over the tokens whose
+//     weights a lane already has: it reads piece r of those 4 tokens (16 bytes), converts, and pairs tokens by byte permutation.
+//     Lane (r, g) receives numbers 8 (4 g + i) + j of row r.
+// So a row's maximum, sum and correction are one register, the same for all of a lane's scores and results.
+#include "mx4.h"
+
+namespace gs {
+
+namespace {
+
+constexpr int kTile = 64;            // tokens of a wave's step
+constexpr int kWaves = 4;
+constexpr int kMinTiles = 8;         // of a part: two per wave
+constexpr int kMaxParts = 64;        // the joining kernel has a lane for each
+// Weights are 2^(score - maximum - kHeadroom): their sum over 2^24 tokens, times the largest number of the format, does not
+// overflow before it is divided by their sum.
+constexpr float kHeadroom = 24.0f;
+
+// What the rows row0 .. row1 of a sequence of `len` tokens have to look at, in tiles: the first `sink_tiles`, then
+// those from `window_tile` on.  Cut into parts of `per` tiles.
+struct Span {
+  int32_t hi;                        // tokens from here on are seen by no row
+  int32_t sink_tiles, window_tile, total, per, parts;
+  __device__ int32_t token(int32_t i) const { return (i < sink_tiles ? i : window_tile + i - sink_tiles) * kTile; }
+};
+__device__ __forceinline__ Span span_of(const Mx4AttendArgs& a, int32_t len, int32_t row0, int32_t row1) {
+  Span s;
+  const int32_t first = len - a.queries + row0 / a.group, last = len - a.queries + row1 / a.group;    // positions
+  s.hi = last + 1 > 0 ? last + 1 : 0;
+  int32_t lo = 0;
+  if (a.window > 0 && first >= a.window) lo = first - int32_t(a.window) + 1;
+  const int32_t sinks = a.sinks < lo ? int32_t(a.sinks) : lo;
+  s.sink_tiles = (sinks + kTile - 1) / kTile;
+  s.window_tile = lo / kTile > s.sink_tiles ? lo / kTile : s.sink_tiles;
+  const int32_t end = (s.hi + kTile - 1) / kTile;
+  s.total = s.sink_tiles + (end > s.window_tile ? end - s.window_tile : 0);
+  s.per = (s.total + a.parts - 1) / a.parts;
+  s.per = s.per > kMinTiles ? s.per : kMinTiles;
+  s.parts = s.total > s.per ? (s.total + s.per - 1) / s.per : 1;
+  return s;
+}
+__device__ __forceinline__ int32_t length_of(const Mx4AttendArgs& a, int64_t b) {
+  const int32_t len = a.lengths[b], most = int32_t(a.width) * a.cache.page;
+  return len < 0 ? 0 : len < most ? len : most;
+}
+
+// Maximum and sum over the four lanes that have the same r.
+__device__ __forceinline__ float max_over_g(float v) {
+  uint32_t u = __float_as_uint(v);
+  auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  u = __float_as_uint(v);
+  p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_over_g(float v) {
+  uint32_t u = __float_as_uint(v);
+  auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  u = __float_as_uint(v);
+  p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// N dwords from an address aligned to 4 bytes (8 where N is even, 16 where it is a multiple of 4).
+template <int N>
+__device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&out)[N]) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const i32x4 v = reinterpret_cast<const i32x4*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[4 * i + j] = uint32_t(v[j]);
+    }
+  } else if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const i32x2 v = reinterpret_cast<const i32x2*>(p)[i];
+      out[2 * i] = uint32_t(v[0]);
+      out[2 * i + 1] = uint32_t(v[1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = reinterpret_cast<const uint32_t*>(p)[i];
+  }
+}
+
+template <int D, int QT>
+struct AttendShape {
+  static constexpr int C = D / 32;                       // blocks of 32; dwords of a lane's quarter of a key
+  static constexpr int KS = (C == 2 || C == 4) ? 1 : 2;  // scale bytes that this quarter has
+  static constexpr int VP = (D / 8 + 15) / 16;           // passes over the pieces of the values, 16 at a time
+  static constexpr int kRow = D + 4;                     // floats of a row while waves are joined
+  static constexpr int kRows = 16 * QT;
+  static constexpr size_t kLds = size_t(kWaves) * 16 * (kRow + 2) * 4;
+};
+
+template <int D, int QT>
+__global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a) {
+  using S = AttendShape<D, QT>;
+  constexpr int C = S::C, KS = S::KS, VP = S::VP, kRows = S::kRows, kRow = S::kRow;
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  // workgroup -> (sequence and cache head, row tile, part)
+  const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
+  uint32_t at = blockIdx.x;
+  const uint32_t part = at % uint32_t(a.parts);
+  at /= uint32_t(a.parts);
+  const uint32_t row_tile = at % uint32_t(row_tiles), bh = at / uint32_t(row_tiles);
+  const uint32_t b = bh / uint32_t(a.cache.heads), head = bh - b * uint32_t(a.cache.heads);
+  const int32_t row0 = int32_t(row_tile) * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
+  const int32_t len = length_of(a, b);
+  const Span span = span_of(a, len, row0, row1);
+  if (int32_t(part) >= span.parts) return;
+  const int32_t begin = int32_t(part) * span.per, stop = begin + span.per < span.total ? begin + span.per : span.total;
+
+  // the rows' queries, as the scores' products want them, and positions
+  i32x4 q[QT][C];
+  int32_t pos[QT];
+  const int64_t q_row = int64_t(a.cache.heads) * a.group * D;       // elements of one query position
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int32_t row = row0 + t * 16 + r;
+    const int32_t i = row / a.group, h = row - i * a.group;
+    const bool ok = row < rows;
+    pos[t] = ok ? len - a.queries + i : -1;
+    const uint16_t* src = static_cast<const uint16_t*>(a.q) + (int64_t(b) * a.queries + i) * q_row + (int64_t(head) * a.group + h) * D + g * (D / 4);
+#pragma unroll
+    for (int c = 0; c < C; ++c) q[t][c] = ok ? *reinterpret_cast<const i32x4*>(src + 8 * c) : i32x4{0, 0, 0, 0};
+  }
+  const int32_t pos_first = len - a.queries + row0 / a.group, pos_last = len - a.queries + row1 / a.group;
+  const float to_log2 = a.scale * 1.44269504088896340736f;
+
+  f32x4 o[QT][VP][8];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -__builtin_inff();
+    l[t] = 0;
+#pragma unroll
+    for (int p = 0; p < VP; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[t][p][j] = f32x4{0, 0, 0, 0};
+  }
+
+  struct Tile {
+    uint32_t k[4][C], ks[4][KS], vs[4][VP];
+    i32x4 v[4][VP];
+    int32_t token;
+    uint32_t there;                  // bit i: tokens 16 i .. of the tile are in a page
+  };
+  const int32_t* table = a.table + int64_t(b) * a.width;
+  auto page_of = [&](int32_t token, uint32_t* slot) -> int32_t {    // wave-uniform; below zero: none
+    if (token >= span.hi) return -1;
+    uint32_t entry;
+    a.cache.by_page.divmod(uint32_t(token), &entry, slot);
+    const int32_t id = table[entry];
+    return id < a.cache.n_pages ? id : -1;
+  };
+  auto load = [&](int32_t i, Tile& t) {
+    t.token = span.token(i);
+    t.there = 0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      uint32_t slot = 0;
+      const int32_t id = page_of(t.token + 16 * n, &slot);
+      if (id >= 0) {
+        t.there |= 1u << n;
+        const uint8_t* blk = a.cache.block(id, int(head));
+        load_dwords<C>(blk + slot * (D / 2) + uint32_t(r * (D / 2) + g * (D / 8)), t.k[n]);
+        const uint8_t* ks = blk + uint32_t(a.cache.page) * D + slot * C + uint32_t(r * C);
+        t.ks[n][0] = ks[(C * g) / 4];
+        if constexpr (KS == 2) t.ks[n][1] = ks[(C * g + C - 1) / 4];
+#pragma unroll
+        for (int p = 0; p < VP; ++p) {
+          const int piece = 16 * p + r;
+          const bool ok = D / 8 - 16 * p >= 16 || piece < D / 8;
+          t.v[n][p] = i32x4{0, 0, 0, 0};
+          t.vs[n][p] = 0x7f7f7f7fu;
+          if (ok) {
+            t.v[n][p] = *reinterpret_cast<const i32x4*>(blk + uint32_t(a.cache.page) * (D / 2) + (slot / 4 + g) * (D * 2) + piece * 16);
+            t.vs[n][p] = *reinterpret_cast<const uint32_t*>(blk + uint32_t(a.cache.page) * (D + C) + ((slot / 4 + g) * C + piece / 4) * 4);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) t.k[n][c] = 0;
+#pragma unroll
+        for (int c = 0; c < KS; ++c) t.ks[n][c] = 127;
+#pragma unroll
+        for (int p = 0; p < VP; ++p) {
+          t.v[n][p] = i32x4{0, 0, 0, 0};
+          t.vs[n][p] = 0x7f7f7f7fu;
+        }
+      }
+    }
+  };
+  auto sees = [&](int32_t position, int32_t token) {
+    return token <= position && (a.window == 0 || position - token < a.window || token < a.sinks);
+  };
+
+  auto compute = [&](const Tile& t) {
+    // scores: s[row tile][run of 16 tokens]
+    f32x4 s[QT][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      float sc[KS];
+#pragma unroll
+      for (int c = 0; c < KS; ++c) sc[c] = mx4_scale(t.ks[n][c]);
+      i32x4 kv[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) kv[c] = mx4_decode8(t.k[n][c], KS == 1 || (C * g + c) / 4 == (C * g) / 4 ? sc[0] : sc[KS - 1]);
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv[c]), __builtin_bit_cast(bf16x8, q[u][c]), acc, 0, 0, 0);
+        s[u][n] = acc;
+      }
+    }
+    const bool all_seen = t.there == 15 && t.token + kTile - 1 <= pos_first &&
+                          (a.window == 0 || pos_last - t.token < a.window || t.token + kTile <= a.sinks);
+    // weights, as the products with the values want them: p[row tile][half of the tile]
+    i32x4 w[QT][2];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      float e[16];
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[4 * n + i] = s[u][n][i] * to_log2;
+      if (!all_seen) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!((t.there >> n) & 1) || !sees(pos[u], t.token + 16 * n + 4 * g + i)) e[4 * n + i] = -__builtin_inff();
+      }
+      float top = e[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, e[i]);
+      top = fmaxf(max_over_g(top) + kHeadroom, m[u]);
+      const float ref = top == -__builtin_inff() ? 0.0f : top;
+      if (__any(top > m[u])) {
+        const float shrink = exp2_fast(m[u] - ref);
+        m[u] = top;
+        l[u] *= shrink;
+#pragma unroll
+        for (int p = 0; p < VP; ++p)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[u][p][j] *= shrink;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] = exp2_fast(e[i] - ref);
+      float sum = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum += e[i];
+      l[u] += sum;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[u][h][i] = int32_t(pack_bf16x2(e[8 * h + 2 * i], e[8 * h + 2 * i + 1]));
+    }
+    // scale bytes of 253 and more (2^126, 2^127, NaN) could make infinities or NaN of a number; times a weight of zero that would
+    // spoil rows that do not see the token
+    uint32_t wild = 0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int p = 0; p < VP; ++p) wild |= ((t.vs[n][p] & 0x7f7f7f7fu) + 0x03030303u) & t.vs[n][p];
+    const bool tame = !__any((wild & 0x80808080u) != 0);
+    auto values = [&](int h, int p, const float (&sc)[8], bool keep, i32x4 (&va)[8]) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {             // pairs of tokens of one run of 16
+        const i32x4 raw = t.v[2 * h + half][p];
+        uint32_t d[4][4];                                // [token][pair of numbers]
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t x = keep ? uint32_t(raw[j]) : 0u;
+          const i32x4 y = mx4_decode8(x, sc[4 * half + j]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) d[j][c] = uint32_t(y[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            va[2 * c][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x05040100u));
+            va[2 * c + 1][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x07060302u));
+          }
+      }
+    };
+    if (tame) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int p = 0; p < VP; ++p) {
+          float sc[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t x = ((t.vs[2 * h + j / 4][p] >> (8 * (j % 4))) & 255u) << 23;
+            sc[j] = __uint_as_float(x > 0x00400000u ? x : 0x00400000u);
+          }
+          i32x4 va[8];
+          values(h, p, sc, true, va);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+              o[u][p][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[j]), __builtin_bit_cast(bf16x8, w[u][h]),
+                                                                   o[u][p][j], 0, 0, 0);
+        }
+    } else {
+      // block by block of 32 numbers: the scales go to the weights of the tokens that a row sees
+      const float one[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll 1
+      for (int blk = 0; blk < C; ++blk) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t bytes[2];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t slot = 0;
+            const int32_t id = page_of(t.token + 16 * (2 * h + half), &slot);
+            bytes[half] = 0x7f7f7f7fu;
+            if (id >= 0)
+              bytes[half] = *reinterpret_cast<const uint32_t*>(a.cache.block(id, int(head)) + uint32_t(a.cache.page) * (D + C) +
+                                                               ((slot / 4 + g) * C + blk) * 4);
+          }
+          i32x4 scaled[QT];
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float f[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int n = 2 * h + i / 2, j = 2 * (i % 2) + k;      // run of 16, token of the lane's four
+                const float weight = __uint_as_float(k ? uint32_t(w[u][h][i]) & 0xffff0000u : uint32_t(w[u][h][i]) << 16);
+                const bool seen = ((t.there >> n) & 1) && sees(pos[u], t.token + 16 * n + 4 * g + j);
+                f[k] = seen ? weight * mx4_scale((bytes[i / 2] >> (8 * j)) & 255u) : 0.0f;
+              }
+              scaled[u][i] = int32_t(pack_bf16x2(f[0], f[1]));
+            }
+#pragma unroll
+          for (int p = 0; p < VP; ++p) {
+            i32x4 va[8];
+            values(h, p, one, (16 * p + r) / 4 == blk, va);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int u = 0; u < QT; ++u) {
+                const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[j]), __builtin_bit_cast(bf16x8, scaled[u]),
+                                                                          f32x4{0, 0, 0, 0}, 0, 0, 0);
+                // lane (r, g) receives piece 16 p + 4 g + i: only those of this block (others are zero, or NaN)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if ((16 * p + 4 * g + i) / 4 == blk) o[u][p][j][i] += add[i];
+              }
+          }
+        }
+      }
+    }
+  };
+
+  for (int32_t i = begin + wave; i < stop; i += kWaves) {
+    Tile t;
+    load(i, t);
+    compute(t);
+  }
+
+  // join the waves, 16 rows at a time
+  float* const my_o = lds + wave * 16 * kRow;
+  float* const ml = lds + kWaves * 16 * kRow;            // [wave][row][2]
+  const int64_t task = int64_t(bh) * row_tiles + row_tile;
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    const float sum = sum_over_g(l[u]);
+    if (u) __syncthreads();
+    if (g == 0) {
+      ml[(wave * 16 + r) * 2] = m[u];
+      ml[(wave * 16 + r) * 2 + 1] = sum;
+    }
+#pragma unroll
+    for (int p = 0; p < VP; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int piece = 16 * p + 4 * g + i;
+        if (D / 8 - 16 * p >= 16 || piece < D / 8)
+#pragma unroll
+          for (int j = 0; j < 8; j += 4)
+            *reinterpret_cast<f32x4*>(my_o + r * kRow + piece * 8 + j) = f32x4{o[u][p][j][i], o[u][p][j + 1][i], o[u][p][j + 2][i], o[u][p][j + 3][i]};
+      }
+    __syncthreads();
+    const int rr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * 16 + rr) * 2]);
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    float total = 0, f[kWaves];
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      f[v] = exp2_fast(ml[(v * 16 + rr) * 2] - ref);
+      total += f[v] * ml[(v * 16 + rr) * 2 + 1];
+    }
+    float x[D / 16];
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+      x[d] = 0;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) x[d] += f[v] * lds[(v * 16 + rr) * kRow + d0 + d];
+    }
+    const int32_t row = row0 + u * 16 + rr;
+    if (row >= rows) continue;
+    if (span.parts == 1) {
+      const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+      const int32_t i = row / a.group, h = row - i * a.group;
+      const int64_t dst = (int64_t(b) * a.queries + i) * q_row + (int64_t(head) * a.group + h) * D + d0;
+#pragma unroll
+      for (int d = 0; d < D / 16; d += 2) {
+        if (a.out_dtype == GS_BF16)
+          *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + dst + d) = pack_bf16x2(x[d] * inv, x[d + 1] * inv);
+        else
+          *reinterpret_cast<f32x2_t*>(static_cast<float*>(a.out) + dst + d) = f32x2_t{x[d] * inv, x[d + 1] * inv};
+      }
+    } else {
+      const int64_t slot = (task * a.parts + part) * kRows + u * 16 + rr;
+      float* dst = a.partial + slot * (D + 2);
+      if (d0 == 0) {
+        dst[0] = top;
+        dst[1] = total;
+      }
+#pragma unroll
+      for (int d = 0; d < D / 16; d += 2) *reinterpret_cast<f32x2_t*>(dst + 2 + d0 + d) = f32x2_t{x[d], x[d + 1]};
+    }
+  }
+}
+
+// Joins the parts of a row: one wave per row, a lane for each part's maximum and sum, then two numbers per lane.
+template <int D, int QT>
+__global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, int64_t total_rows) {
+  constexpr int kRows = 16 * QT;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total_rows) return;
+  const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
+  const int64_t bh = at / rows;
+  const int32_t row = int32_t(at - bh * rows), row_tile = row / kRows;
+  const int64_t b = bh / a.cache.heads;
+  const int head = int(bh - b * a.cache.heads);
+  const int32_t row0 = row_tile * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
+  const Span span = span_of(a, length_of(a, b), row0, row1);
+  if (span.parts == 1) return;
+  const float* src = a.partial + ((bh * row_tiles + row_tile) * a.parts * kRows + (row - row0)) * (D + 2);
+  constexpr int64_t kStride = int64_t(kRows) * (D + 2);
+  float m = -__builtin_inff(), l = 0;
+  if (lane < span.parts) {
+    m = src[lane * kStride];
+    l = src[lane * kStride + 1];
+  }
+  float top = m;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
+  const float f = exp2_fast(m - (top == -__builtin_inff() ? 0.0f : top));
+  float total = lane < span.parts ? f * l : 0.0f;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
+  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+  const int32_t i = row / a.group, h = row - i * a.group;
+  const int64_t dst = ((b * a.queries + i) * a.cache.heads * a.group + int64_t(head) * a.group + h) * D;
+#pragma unroll
+  for (int d0 = 0; d0 < D; d0 += 128) {
+    const int d = d0 + 2 * lane;
+    float x0 = 0, x1 = 0;
+    for (int p = 0; p < span.parts; ++p) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), p));
+      if (d < D) {
+        const f32x2_t v = *reinterpret_cast<const f32x2_t*>(src + p * kStride + 2 + d);
+        x0 += w * v[0];
+        x1 += w * v[1];
+      }
+    }
+    if (d < D) {
+      if (a.out_dtype == GS_BF16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + dst + d) = pack_bf16x2(x0 * inv, x1 * inv);
+      else *reinterpret_cast<f32x2_t*>(static_cast<float*>(a.out) + dst + d) = f32x2_t{x0 * inv, x1 * inv};
+    }
+  }
+}
+
+// Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
+void plan(Mx4AttendArgs* a) {
+  const int64_t rows = int64_t(a->queries) * a->group;
+  a->tiles = rows > 16 ? 2 : 1;
+  const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles);
+  int64_t most = a->width * a->cache.page;
+  if (a->window > 0) {
+    const int64_t seen = a->window + a->queries + (a->sinks < most ? a->sinks : most) + 2 * kTile;
+    most = seen < most ? seen : most;
+  }
+  int64_t parts = ceil_div(1024, tasks > 0 ? tasks : 1);
+  const int64_t useful = ceil_div(ceil_div(most, kTile), kMinTiles);
+  parts = parts < useful ? parts : useful;
+  parts = parts < kMaxParts ? parts : kMaxParts;
+  a->parts = int32_t(parts > 1 ? parts : 1);
+}
+
+template <int D, int QT>
+hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
+  using S = AttendShape<D, QT>;
+  const int64_t rows = int64_t(a.queries) * a.group;
+  const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, S::kRows) * a.parts;
+  const int64_t total_rows = a.batch * a.cache.heads * rows;
+  if (groups > 0x7fffffff || total_rows > 0x7fffffff) return hipErrorInvalidValue;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mx4_attend_kernel<D, QT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, int(S::kLds));
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((mx4_attend_kernel<D, QT>), dim3(unsigned(groups)), dim3(kWaves * 64), S::kLds, s, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.parts > 1) {
+    hipLaunchKernelGGL((mx4_attend_join_kernel<D, QT>), dim3(unsigned(ceil_div(total_rows, 4))), dim3(256), 0, s, a, total_rows);
+    e = hipGetLastError();
+  }
+  return e;
+}
+template <int D>
+hipError_t launch_d(const Mx4AttendArgs& a, hipStream_t s) {
+  return a.tiles == 1 ? launch<D, 1>(a, s) : launch<D, 2>(a, s);
+}
+
+}  // namespace
+
+size_t mx4_attend_workspace(const Mx4AttendArgs& given) {
+  Mx4AttendArgs a = given;
+  plan(&a);
+  if (a.parts == 1) return 0;
+  const int64_t rows = int64_t(a.queries) * a.group;
+  return size_t(a.batch * a.cache.heads * ceil_div(rows, 16 * a.tiles) * a.parts * 16 * a.tiles) * size_t(a.cache.dim + 2) * 4;
+}
+
+hipError_t launch_mx4_attend(const Mx4AttendArgs& given, hipStream_t s) {
+  Mx4AttendArgs a = given;
+  plan(&a);
+  if (a.batch == 0 || a.queries == 0 || a.group == 0) return hipSuccess;
+  switch (a.cache.dim) {
+    case 64: return launch_d<64>(a, s);
+    case 96: return launch_d<96>(a, s);
+    case 128: return launch_d<128>(a, s);
+    case 192: return launch_d<192>(a, s);
+    case 256: return launch_d<256>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace gs

@@ -1,0 +1,206 @@
+// Conversion to and from microscaled 4-bit floats: whole matrices, and tokens of a paged cache.
+//
+// A scale is the power of two of its block's largest magnitude, over 4 (the largest power of two of e2m1),
+// so a block is read once, reduced over its 32 numbers, and written: 8 numbers per lane, four neighbouring lanes per block,
+// the maximum over them by two lane exchanges.  Bound by memory: n numbers of s bytes move n (s + 17/32).
+#include "mx4.h"
+
+namespace gs {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ float load_plain(const void* p, int64_t i, std::integral_constant<int, GS_BF16>) {
+  return bf16_bits_to_float(static_cast<const uint16_t*>(p)[i]);
+}
+__device__ __forceinline__ float load_plain(const void* p, int64_t i, std::integral_constant<int, GS_F32>) {
+  return static_cast<const float*>(p)[i];
+}
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight numbers of a row from element `at` on, zero beyond `left` of them.
+template <int DT>
+__device__ __forceinline__ void load8(const void* row, int64_t at, int64_t left, float (&x)[8]) {
+  if (left >= 8) {
+    if constexpr (DT == GS_BF16) {
+      const i32x4 v = *reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(uint32_t(v[i]) << 16);
+        x[2 * i + 1] = __uint_as_float(uint32_t(v[i]) & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4_any v = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * h + i] = v[i];
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < left ? load_plain(row, at + i, std::integral_constant<int, DT>{}) : 0.0f;
+}
+
+template <int DT>
+__device__ __forceinline__ void store8(void* row, int64_t at, int64_t left, uint32_t w, float scale) {
+  if constexpr (DT == GS_BF16) {
+    uint16_t* dst = static_cast<uint16_t*>(row) + at;
+    const i32x4 v = mx4_decode8(w, scale);
+    if (left >= 8) {
+      *reinterpret_cast<i32x4_any2*>(dst) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < left) dst[i] = uint16_t(uint32_t(v[i / 2]) >> (16 * (i & 1)));
+    }
+  } else {
+    float* dst = static_cast<float*>(row) + at;
+    float x[8];
+    mx4_decode2_f32<0>(w, scale, x);
+    mx4_decode2_f32<1>(w, scale, x + 2);
+    mx4_decode2_f32<2>(w, scale, x + 4);
+    mx4_decode2_f32<3>(w, scale, x + 6);
+    if (left >= 8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4_any*>(dst + 4 * h) = f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < left) dst[i] = x[i];
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t block_scale_byte(const float (&x)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+    top = top > b ? top : b;
+  }
+  return mx4_scale_byte(max_of_4_lanes(top));
+}
+
+// A row's pieces of 8 numbers are counted up to whole runs of scale bytes (`per_row`, a multiple of 32), the padding
+// written as zeros by the same lanes.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a, int64_t per_row, int64_t total) {
+  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols);
+  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
+    const int64_t row = at / per_row, piece = at - row * per_row;
+    float x[8];
+    const void* src = static_cast<const uint8_t*>(a.plain) + row * a.cols * int64_t(dtype_size(DT));
+    load8<DT>(src, piece * 8, a.cols - piece * 8, x);
+    const uint32_t byte = block_scale_byte(x);
+    const int64_t block = piece / 4;
+    if (block < blocks) static_cast<uint32_t*>(a.values)[row * blocks * 4 + piece] = mx4_encode8(x, byte);
+    if (piece % 4 == 0) static_cast<uint8_t*>(a.scales)[row * pitch + block] = uint8_t(block < blocks ? byte : 0);
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs a, int64_t per_row, int64_t total) {
+  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols);
+  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
+    const int64_t row = at / per_row, piece = at - row * per_row;
+    const uint32_t w = static_cast<const uint32_t*>(a.values)[row * blocks * 4 + piece];
+    const uint32_t byte = static_cast<const uint8_t*>(a.scales)[row * pitch + piece / 4];
+    void* dst = static_cast<uint8_t*>(a.plain) + row * a.cols * int64_t(dtype_size(DT));
+    store8<DT>(dst, piece * 8, a.cols - piece * 8, w, mx4_scale(byte));
+  }
+}
+
+unsigned grid_for(int64_t total) {
+  const int64_t n = ceil_div(total, kThreads);
+  return unsigned(n < 256 * 64 ? n : 256 * 64);
+}
+
+// Lanes run over (batch, token, head, piece of 8 numbers); blockIdx.y: keys or values.
+struct Token {
+  uint8_t* block;         // null: no place in the cache
+  uint32_t slot;
+};
+__device__ __forceinline__ Token place_of(const Mx4TokenArgs& a, int64_t b, int64_t t, int head, bool counted) {
+  Token k{nullptr, 0};
+  if (counted && a.counts && t >= a.counts[b]) return k;
+  const int64_t pos = int64_t(a.first[b]) + t;
+  if (pos < 0 || pos >= a.width * a.cache.page) return k;
+  uint32_t entry;
+  a.cache.by_page.divmod(uint32_t(pos), &entry, &k.slot);
+  const int32_t id = a.table[b * a.width + entry];
+  if (id < 0 || id >= a.cache.n_pages) return k;
+  k.block = a.cache.block(id, head);
+  return k;
+}
+
+template <int DT, bool WRITE>
+__global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, int64_t total) {
+  const uint32_t pieces = uint32_t(a.cache.dim / 8);
+  const bool values = blockIdx.y;
+  void* plain = values ? a.v : a.k;
+  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
+    int64_t r = at / pieces;
+    const uint32_t piece = uint32_t(at - r * pieces);
+    const int64_t token = r / a.cache.heads;
+    const int head = int(r - token * a.cache.heads);
+    const int64_t b = token / a.tokens, t = token - b * a.tokens;
+    const Token place = place_of(a, b, t, head, WRITE);
+    const uint32_t codes = values ? a.cache.value(place.slot, piece) : a.cache.key(place.slot) + piece * 4;
+    const uint32_t scale = values ? a.cache.value_scale(place.slot, piece / 4) : a.cache.key_scale(place.slot, piece / 4);
+    if constexpr (WRITE) {
+      float x[8];
+      load8<DT>(plain, at * 8, 8, x);
+      const uint32_t byte = block_scale_byte(x);
+      if (place.block) {
+        *reinterpret_cast<uint32_t*>(place.block + codes) = mx4_encode8(x, byte);
+        if (piece % 4 == 0) place.block[scale] = uint8_t(byte);
+      }
+    } else {
+      uint32_t w = 0;
+      float s = 1.0f;
+      if (place.block) {
+        w = *reinterpret_cast<const uint32_t*>(place.block + codes);
+        s = mx4_scale(place.block[scale]);
+      }
+      store8<DT>(plain, at * 8, 8, w, s);
+    }
+  }
+}
+
+template <bool WRITE>
+hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {
+  const int64_t total = a.batch * a.tokens * a.cache.heads * (a.cache.dim / 8);
+  if (total == 0) return hipSuccess;
+  const dim3 grid(grid_for(total), 2);
+  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_tokens_kernel<GS_BF16, WRITE>), grid, dim3(kThreads), 0, s, a, total);
+  else hipLaunchKernelGGL((mx4_tokens_kernel<GS_F32, WRITE>), grid, dim3(kThreads), 0, s, a, total);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quantize(const Mx4ConvertArgs& a, hipStream_t s) {
+  const int64_t per_row = mx4_scale_pitch(a.cols) * 4, total = a.rows * per_row;
+  if (total == 0) return hipSuccess;
+  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_quantize_kernel<GS_BF16>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
+  else hipLaunchKernelGGL((mx4_quantize_kernel<GS_F32>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_dequantize(const Mx4ConvertArgs& a, hipStream_t s) {
+  const int64_t per_row = ceil_div(a.cols, 8), total = a.rows * per_row;
+  if (total == 0) return hipSuccess;
+  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_dequantize_kernel<GS_BF16>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
+  else hipLaunchKernelGGL((mx4_dequantize_kernel<GS_F32>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_append(const Mx4TokenArgs& a, hipStream_t s) { return launch_tokens<true>(a, s); }
+hipError_t launch_mx4_read(const Mx4TokenArgs& a, hipStream_t s) { return launch_tokens<false>(a, s); }
+
+}  // namespace gs
