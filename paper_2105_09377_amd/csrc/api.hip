@@ -1,7 +1,7 @@
 // C ABI of the library: host-side validation of the access-pattern shape rules (Table 1, Table 2,
 // Fig. 2, Fig. 5) and dispatch to the kernels.  Everything is checked before anything is
 // launched, so every error path can be exercised on a host without a GPU.
-#include "common.h"
+#include "checks.h"
 
 #include <limits.h>
 #include <string.h>

@@ -239,11 +239,6 @@ __device__ __forceinline__ void store_result(void* out, const void* residual, in
   }
 }
 
-// What the entry points share (api.hip): the structural check of an access pattern, of its pointer too where kernels
-// will follow it, and the status of a launch.
-int check_ap(const gs_ap* a, bool need_data);
-int launch_status(hipError_t e);
-
 // ---------------------------------------------------------------------------------------------
 // Kernel launchers (defined in the .hip files).  All return hipError_t from the launch.
 // ---------------------------------------------------------------------------------------------

@@ -112,6 +112,8 @@ struct Mx4DotArgs {       // out[m][n] = sum_k x[m][k] w[n][k]
   void* out;
   int out_dtype, relu;
   int64_t M, N, K;
+  int32_t splits;         // set by the launcher: workgroups that share the sum over K of a tile; above 1, `out` has as many
+                          // results in fp32, one after the other
 };
 hipError_t launch_mx4_dot(const Mx4DotArgs& a, void* workspace, hipStream_t s);
 size_t mx4_dot_workspace(bool x_is_bf16, int64_t M, int64_t N, int64_t K);

@@ -1,5 +1,6 @@
 // Entry points on microscaled 4-bit floats: host-side checks and dispatch.  Everything is checked before anything is
 // launched.
+#include "checks.h"
 #include "mx4.h"
 
 #include <limits.h>

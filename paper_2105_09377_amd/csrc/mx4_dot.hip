@@ -5,35 +5,56 @@
 // The order in which K is summed is free as long as both operands have the same one.  A unit is 8 blocks (256 of K)
 // of 16 rows: lane (r = lane % 16, g = lane / 16) holds blocks 2 g and 2 g + 1 of row r, 32 consecutive bytes, and the
 // two scale bytes beside each other.
-#include "mx4.h"
+#include "mx4_weight_tile.h"
 
 namespace gs {
 
 namespace {
 
-typedef int32_t i32x8v __attribute__((ext_vector_type(8)));
-typedef int32_t i32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ f32x4 mfma_mx4(const i32x4& a, const i32x4& b, const f32x4& c, int sa, int sb, std::integral_constant<int, 0>) {
-  const i32x8v x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  const i32x8t x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, sa, 0, sb);
 }
 __device__ __forceinline__ f32x4 mfma_mx4(const i32x4& a, const i32x4& b, const f32x4& c, int sa, int sb, std::integral_constant<int, 1>) {
-  const i32x8v x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  const i32x8t x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 1, sa, 1, sb);
 }
 
+typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+
 // ---------------------------------------------------------------------------------------------
 // Few rows of x: NW waves share a tile of 16 MT rows of x and 16 NT rows of w, the units of K dealt to them, their
-// partial tiles added at the end.  Everything is loaded where it is used: w is read once for each 16 MT rows of x.
+// partial tiles added at the end in the order of the waves.  Everything goes from memory to registers, the next unit's
+// loads in flight while one is multiplied: w is read once, and bound by that.
 // ---------------------------------------------------------------------------------------------
 template <bool XBF, int MT, int NT, int NW>
-__global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, int64_t tiles_n) {
+__global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uint32_t tiles_n) {
   __shared__ f32x4 part[NW][MT * NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int64_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int64_t m0 = tm * 16 * MT, n0 = tn * 16 * NT;
-  const int64_t nb = mx4_blocks(a.K), pitch = mx4_scale_pitch(a.K), units = pitch / 8;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
+  const int64_t m0 = int64_t(tm) * 16 * MT, n0 = int64_t(tn) * 16 * NT;
+  const int64_t nb = mx4_blocks(a.K), pitch = mx4_scale_pitch(a.K);
+  const int32_t units = int32_t(pitch / 8);
+
+  // a lane's rows; those behind the end are the last one, and their results are not stored
+  const uint8_t *wp[NT], *wsp[NT], *xp[MT], *xsp[MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t row = n0 + n * 16 + r < a.N ? n0 + n * 16 + r : a.N - 1;
+    wp[n] = static_cast<const uint8_t*>(a.w) + row * nb * 16 + g * 32;
+    wsp[n] = a.ws + row * pitch + g * 2;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int64_t row = m0 + m * 16 + r < a.M ? m0 + m * 16 + r : a.M - 1;
+    if constexpr (XBF) {
+      xp[m] = static_cast<const uint8_t*>(a.x) + (row * a.K + g * 64) * 2;
+    } else {
+      xp[m] = static_cast<const uint8_t*>(a.x) + row * nb * 16 + g * 32;
+      xsp[m] = a.xs + row * pitch + g * 2;
+    }
+  }
 
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -41,68 +62,98 @@ __global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, int
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
 
-  for (int64_t u = wave; u < units; u += NW) {
-    i32x4 w[NT][2];
-    uint32_t wsc[NT];
+  constexpr int XP = XBF ? 8 : 2;          // 16-byte pieces of a lane's two blocks of x
+  struct Unit {
+    i32x4 w[NT][2], x[MT][XP];
+    uint32_t ws[NT], xs[MT];
+  };
+  auto load = [&](int32_t u, Unit& t) {
+    // blocks behind K are read as zeros
+    const int64_t at = int64_t(u) * 8;
+    const bool whole = at + 8 <= nb;       // (uniform)
+    const int32_t left = int32_t(nb - at) - 2 * g;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int64_t row = n0 + n * 16 + r;
-      const bool ok = row < a.N;
-      wsc[n] = ok ? *reinterpret_cast<const uint16_t*>(a.ws + row * pitch + u * 8 + 2 * g) : 0u;
+      t.ws[n] = *reinterpret_cast<const uint16_t*>(wsp[n] + at);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int64_t blk = u * 8 + 2 * g + s;
-        w[n][s] = ok && blk < nb ? static_cast<const i32x4*>(a.w)[row * nb + blk] : i32x4{0, 0, 0, 0};
+        t.w[n][s] = i32x4{0, 0, 0, 0};
+        if (whole || s < left) t.w[n][s] = *reinterpret_cast<const i32x4*>(wp[n] + at * 16 + s * 16);
       }
     }
     if constexpr (!XBF) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const int64_t row = m0 + m * 16 + r;
-        const bool ok = row < a.M;
-        const uint32_t xsc = ok ? *reinterpret_cast<const uint16_t*>(a.xs + row * pitch + u * 8 + 2 * g) : 0u;
-        i32x4 x[2];
+        t.xs[m] = *reinterpret_cast<const uint16_t*>(xsp[m] + at);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const int64_t blk = u * 8 + 2 * g + s;
-          x[s] = ok && blk < nb ? static_cast<const i32x4*>(a.x)[row * nb + blk] : i32x4{0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[m][n] = mfma_mx4(w[n][0], x[0], acc[m][n], int(wsc[n]), int(xsc), std::integral_constant<int, 0>{});
-          acc[m][n] = mfma_mx4(w[n][1], x[1], acc[m][n], int(wsc[n]), int(xsc), std::integral_constant<int, 1>{});
+          t.x[m][s] = i32x4{0, 0, 0, 0};
+          if (whole || s < left) t.x[m][s] = *reinterpret_cast<const i32x4*>(xp[m] + at * 16 + s * 16);
         }
       }
     } else {
+      const int64_t numbers = a.K - at * 32 - g * 64;     // of the lane's part of this row
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int64_t k0 = (u * 8 + 2 * g + s) * 32;
+      for (int m = 0; m < MT; ++m)
+        if (m == 0 || m0 + m * 16 < a.M) {                // (uniform)
+          if (at * 32 + 256 <= a.K) {                     // (uniform)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          i32x4 wv[NT];
+            for (int c = 0; c < 8; ++c) t.x[m][c] = *reinterpret_cast<const i32x4_any2t*>(xp[m] + at * 64 + c * 16);
+          } else {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) wv[n] = mx4_decode8(uint32_t(w[n][s][c]), mx4_scale((wsc[n] >> (8 * s)) & 255u));
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const int64_t row = m0 + m * 16 + r, k = k0 + 8 * c;
-            const uint16_t* src = static_cast<const uint16_t*>(a.x) + row * a.K + k;
-            i32x4 x = {0, 0, 0, 0};
-            if (row < a.M && k < a.K) {
-              if (k + 8 <= a.K) {
-                x = *reinterpret_cast<const i32x4_any2*>(src);
+            for (int c = 0; c < 8; ++c) {
+              t.x[m][c] = i32x4{0, 0, 0, 0};
+              const uint16_t* src = reinterpret_cast<const uint16_t*>(xp[m] + at * 64) + c * 8;
+              if (c * 8 + 8 <= numbers) {
+                t.x[m][c] = *reinterpret_cast<const i32x4_any2t*>(src);
               } else {
 #pragma unroll
                 for (int e = 0; e < 7; ++e)
-                  if (k + e < a.K) x[e / 2] |= int32_t(uint32_t(src[e]) << (16 * (e & 1)));
+                  if (c * 8 + e < numbers) t.x[m][c][e / 2] |= int32_t(uint32_t(src[e]) << (16 * (e & 1)));
               }
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[n]), __builtin_bit_cast(bf16x8, x), acc[m][n], 0, 0, 0);
           }
         }
+    }
+  };
+  auto multiply = [&](const Unit& t) {
+    if constexpr (!XBF) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[m][n] = mfma_mx4(t.w[n][0], t.x[m][0], acc[m][n], int(t.ws[n]), int(t.xs[m]), std::integral_constant<int, 0>{});
+          acc[m][n] = mfma_mx4(t.w[n][1], t.x[m][1], acc[m][n], int(t.ws[n]), int(t.xs[m]), std::integral_constant<int, 1>{});
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        float sc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sc[n] = mx4_scale((t.ws[n] >> (8 * s)) & 255u);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_decode8(uint32_t(t.w[n][s][c]), sc[n]));
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+              if (m == 0 || m0 + m * 16 < a.M)
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, t.x[m][4 * s + c]), acc[m][n], 0, 0, 0);
+          }
       }
     }
+  };
+  if (wave < units) {
+    Unit cur, next;
+    load(wave, cur);
+    int32_t u = wave;
+    for (; u + NW < units; u += NW) {
+      load(u + NW, next);
+      multiply(cur);
+      cur = next;
+    }
+    multiply(cur);
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -125,18 +176,160 @@ __global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, int
 template <bool XBF, int MT, int NT, int NW>
 hipError_t launch_rows(const Mx4DotArgs& a, hipStream_t s) {
   const int64_t tiles_m = ceil_div(a.M, 16 * MT), tiles_n = ceil_div(a.N, 16 * NT);
-  if (tiles_m * tiles_n > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((mx4_dot_rows_kernel<XBF, MT, NT, NW>), dim3(unsigned(tiles_m * tiles_n)), dim3(NW * 64), 0, s, a, tiles_n);
+  if (tiles_m * tiles_n > 0x7fffffff || a.K >= (int64_t(1) << 38)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((mx4_dot_rows_kernel<XBF, MT, NT, NW>), dim3(unsigned(tiles_m * tiles_n)), dim3(NW * 64), 0, s, a, uint32_t(tiles_n));
   return hipGetLastError();
+}
+
+// Adds the parts of a sum over K, in their order: four results per lane.
+__global__ void __launch_bounds__(256) mx4_dot_join_kernel(const float* parts, Mx4DotArgs a, int64_t total) {
+  const int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (at >= total) return;
+  if (at + 4 <= total) {
+    f32x4 sum = *reinterpret_cast<const f32x4_any4*>(parts + at);
+    for (int p = 1; p < a.splits; ++p) sum += *reinterpret_cast<const f32x4_any4*>(parts + p * total + at);
+    if (a.relu)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaxf(sum[e], 0.0f);
+    if (a.out_dtype == GS_BF16)
+      *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + at) = i32x2{int32_t(pack_bf16x2(sum[0], sum[1])), int32_t(pack_bf16x2(sum[2], sum[3]))};
+    else *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = sum;
+    return;
+  }
+  for (int64_t i = at; i < total; ++i) {
+    float sum = parts[i];
+    for (int p = 1; p < a.splits; ++p) sum += parts[p * total + i];
+    store_result<float>(a.out, nullptr, a.out_dtype, i, sum, a.relu);
+  }
+}
+
+// Rows of x, K numbers each, at rows of ldx numbers, zeros behind: what transfers of 16 bytes want.
+__global__ void __launch_bounds__(256) mx4_pad_rows_kernel(const uint16_t* x, uint16_t* out, int64_t rows, int64_t K, int64_t ldx) {
+  const int64_t pieces = ldx / 8, total = rows * pieces;
+  for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < total; at += int64_t(gridDim.x) * 256) {
+    const int64_t row = at / pieces, k = (at - row * pieces) * 8;
+    const uint16_t* src = x + row * K + k;
+    i32x4 v = {0, 0, 0, 0};
+    if (k + 8 <= K) {
+      v = *reinterpret_cast<const i32x4_any2t*>(src);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (k + e < K) v[e / 2] |= int32_t(uint32_t(src[e]) << (16 * (e & 1)));
+    }
+    *reinterpret_cast<i32x4*>(out + row * ldx + k) = v;
+  }
+}
+
+// How a product with MX4 weights is done (times in us).
+enum DotWay { kRows1, kRows2, kTile64x64Few, kTile64x64, kTile128x128Few, kTile128x128Long, kTile128x128, kTile256x256,   // two MX4 operands
+              kWeight32x128, kWeight64x64, kWeight64x128, kWeight128x128, kWeight128x256 };
+struct DotPlan {
+  DotWay way;
+  int splits;            // workgroups that share the sum of a tile
+  int64_t ldx;           // bfloat16 x in tiles: numbers between rows
+  bool pad;              // into the workspace first
+  size_t pad_bytes, part_bytes;
+};
+int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * ceil_div(N, bn); }
+
+DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
+  DotPlan p = {kRows1, 1, 0, false, 0, 0};
+  // Up to 16 rows w is read once by the rows kernel.  Two blocks of 16 columns per wave where that leaves a workgroup for every
+  // compute unit (1 x 8192 x 8192 bf16 10.0 against 11.7 with one; 1 x 4096 x 4096 6.1 against 4.7).  More rows, few tiles: the
+  // waves of a workgroup share K, which a tile walks alone (MX4 100 x 700 x 5000 5.3 against 7.4 in 64x64 tiles, 40 x 300 x 16000
+  // 8.9 / 16.4, 200 x 2000 x 1528 8.2 / 4.2).  bfloat16 rows stand in L2's way where K is long (100 x 700 x 5000 9.2 against 10.1 in
+  // shared tiles, 40 x 300 x 16000 20.3 / 13.1).
+  const int64_t t16x32 = tiles(M, N, 16, 32);
+  p.way = M <= 16 ? (t16x32 >= 256 ? kRows2 : kRows1) : tiles(M, N, 16, 16) > 128 ? kRows2 : kRows1;
+  if (M <= 16 || (t16x32 <= 256 && (!xbf || K <= 6144)) || K == 0 || K > (int64_t(1) << 22)) return p;
+  const int64_t t64 = tiles(M, N, 64, 64), t128 = tiles(M, N, 128, 128);
+  if (!xbf) {
+    // 4096 cubed (256 tiles of 256x256) 39 in those, 47 in 128x128 and 71 in 64x64 tiles; 2048 cubed (64 of them, 256 of 128x128)
+    // 17, 9.7 and 11.3; 1021 x 2000 x 1531 (128 of 128x128) 7.1 and 6.0.  Tiles that a compute unit has for itself are paid for
+    // in latency: more slabs under way (64 x 8192 x 8192 11.3 with four, 18.4 with two), or, where those are few, more waves (2048
+    // cubed 9.7 with eight waves, 10.5 with four; 512 x 8192 x 8192 27.8 and 26.3).
+    if (tiles(M, N, 256, 256) >= 180) p.way = kTile256x256;
+    else if (t128 > 256) p.way = kTile128x128;
+    else if (t128 >= 192) p.way = K > 16 * 256 ? kTile128x128Long : kTile128x128Few;
+    else p.way = t64 <= 256 ? kTile64x64Few : kTile64x64;
+    return p;
+  }
+  p.pad = K % 8 != 0;
+  p.ldx = round_up(K, 8);
+  if (p.pad) p.pad_bytes = size_t(round_up(M * p.ldx * 2, 256));
+  int64_t count = 0;
+  // 2048 x 4096 x 4096 (256 tiles of 128x256) 62.8, 73.9 in 128x128; 512 x 8192 x 8192 (128 of 128x256, 256 of 128x128) 88.8, 68.4,
+  // and 75 in 64x128, 102 in 64x64.
+  if (tiles(M, N, 128, 256) >= 180) p.way = kWeight128x256;
+  else if (t128 >= 160) p.way = kWeight128x128;
+  else if (M <= 32) p.way = kWeight32x128, count = tiles(M, N, 32, 128);
+  else if (t64 > 320) p.way = kWeight64x128;
+  else p.way = kWeight64x64, count = t64;
+  // Fewer tiles than compute units: as many workgroups per tile as fill them, with four slabs each at least (17 x 8192 x 8192 25.8
+  // alone, 17.7, 13.7 and 15.3 by twos, fours and eights; 64 x 8192 x 8192 28.0, 19.9, 20.4, 23.7).
+  if (count > 0 && count < 160) {
+    int64_t splits = (256 + count / 2) / count;
+    const int64_t slabs = ceil_div(K, 128);
+    splits = splits < slabs / 4 ? splits : slabs / 4;
+    splits = splits < 16 ? splits : 16;
+    if (splits > 1) {
+      p.splits = int(splits);
+      p.part_bytes = size_t(splits) * size_t(M) * size_t(N) * 4;
+    }
+  }
+  return p;
 }
 
 }  // namespace
 
-size_t mx4_dot_workspace(bool, int64_t, int64_t, int64_t) { return 0; }
+size_t mx4_dot_workspace(bool x_is_bf16, int64_t M, int64_t N, int64_t K) {
+  const DotPlan p = plan_dot(x_is_bf16, M, N, K);
+  return p.pad_bytes + p.part_bytes;
+}
 
-hipError_t launch_mx4_dot(const Mx4DotArgs& a, void*, hipStream_t s) {
+hipError_t launch_mx4_dot(const Mx4DotArgs& given, void* workspace, hipStream_t s) {
+  Mx4DotArgs a = given;
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  return a.xs ? launch_rows<false, 4, 2, 4>(a, s) : launch_rows<true, 4, 2, 4>(a, s);
+  const DotPlan p = plan_dot(!a.xs, a.M, a.N, a.K);
+  if (p.pad) {
+    const int64_t pieces = a.M * (p.ldx / 8), groups = ceil_div(pieces, 256);
+    hipLaunchKernelGGL(mx4_pad_rows_kernel, dim3(unsigned(groups < 4096 ? groups : 4096)), dim3(256), 0, s, static_cast<const uint16_t*>(a.x),
+                       static_cast<uint16_t*>(workspace), a.M, a.K, p.ldx);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.x = workspace;
+  }
+  void* const parts = static_cast<uint8_t*>(workspace) + p.pad_bytes;
+  Mx4DotArgs b = a;
+  b.splits = p.splits;
+  if (p.splits > 1) {
+    b.out = parts;
+    b.out_dtype = GS_F32;
+    b.relu = 0;
+  }
+  hipError_t e = hipErrorInvalidValue;
+  switch (p.way) {
+    case kRows1: e = a.xs ? launch_rows<false, 1, 1, 8>(a, s) : launch_rows<true, 1, 1, 8>(a, s); break;
+    case kRows2: e = a.xs ? launch_rows<false, 1, 2, 8>(a, s) : launch_rows<true, 1, 2, 8>(a, s); break;
+    case kTile64x64Few: e = launch_mx4_tiles<64, 64, 2, 2, 4>(a, s); break;
+    case kTile64x64: e = launch_mx4_tiles<64, 64, 2, 2, 2>(a, s); break;
+    case kTile128x128Few: e = launch_mx4_tiles<128, 128, 2, 4, 4>(a, s); break;
+    case kTile128x128Long: e = launch_mx4_tiles<128, 128, 2, 2, 4>(a, s); break;
+    case kTile128x128: e = launch_mx4_tiles<128, 128, 2, 2, 2>(a, s); break;
+    case kTile256x256: e = launch_mx4_tiles<256, 256, 2, 4, 2>(a, s); break;
+    case kWeight32x128: e = launch_mx4_weight_tiles<32, 128, 1, 4, 3>(b, p.ldx, s); break;
+    case kWeight64x64: e = launch_mx4_weight_tiles<64, 64, 2, 2, 3>(b, p.ldx, s); break;
+    case kWeight64x128: e = launch_mx4_weight_tiles<64, 128, 2, 2, 2>(b, p.ldx, s); break;
+    case kWeight128x128: e = launch_mx4_weight_tiles<128, 128, 2, 4, 3>(b, p.ldx, s); break;
+    case kWeight128x256: e = launch_mx4_weight_tiles<128, 256, 2, 4, 3>(b, p.ldx, s); break;
+  }
+  if (e != hipSuccess || p.splits == 1) return e;
+  b = a;
+  b.splits = p.splits;
+  const int64_t total = a.M * a.N;
+  hipLaunchKernelGGL(mx4_dot_join_kernel, dim3(unsigned(ceil_div(total, 1024))), dim3(256), 0, s, static_cast<const float*>(parts), b, total);
+  return hipGetLastError();
 }
 
 }  // namespace gs

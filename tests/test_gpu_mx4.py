@@ -129,6 +129,13 @@ PRODUCTS = [(1, 1, 1), (1, 16, 32), (3, 5, 31), (16, 16, 33), (17, 33, 100), (33
             (64, 64, 512), (65, 100, 1000), (100, 31, 8200), (130, 257, 300), (200, 390, 513), (256, 256, 256), (300, 520, 1100), (513, 1024, 96)]
 
 
+# sizes of every way that products are computed, K ending inside slabs and on them, pairs of slabs and single ones
+LARGE = [(3500, 3400, 300), (3400, 3500, 480), (3300, 3600, 512), (2100, 2100, 200), (2050, 2200, 993), (1800, 1800, 700), (1700, 1900, 4400),
+         (1030, 1500, 1531), (1030, 1500, 768), (70, 4000, 8192), (128, 2000, 2049)]
+LARGE_WEIGHTS = [(2300, 2600, 200), (2300, 2600, 201), (1700, 1700, 136), (1700, 1700, 1033), (700, 2200, 300), (700, 2200, 65), (20, 3000, 8000),
+                 (32, 700, 7003), (100, 1500, 7000), (50, 2000, 7001), (300, 1000, 2048), (64, 4000, 1000), (129, 5000, 500)]
+
+
 def operands(m, n, k, seed):
     x, w = normal((m, k), seed, BF, spread=2.0), normal((n, k), seed + 1, BF, spread=2.0)
     return x, w, gs.mx4_quantize(w.to(DEV))
@@ -147,6 +154,37 @@ def test_dot(m, n, k, odt):
     xq = gs.mx4_quantize(x.to(DEV))
     got = gs.mx4_dot(xq, w, out_dtype=odt)
     check_product(got, stored(xq), stored(w))
+
+
+@pytest.mark.parametrize("m,n,k", LARGE)
+def test_dot_in_tiles(m, n, k):
+    x, _, w = operands(m, n, k, 3000 + m + n + k)
+    xq = gs.mx4_quantize(x.to(DEV))
+    check_product(gs.mx4_dot(xq, w, out_dtype=BF if k % 2 else F32), stored(xq), stored(w))
+
+
+@pytest.mark.parametrize("m,n,k", LARGE_WEIGHTS)
+def test_weight_dot_in_tiles(m, n, k):
+    x, _, w = operands(m, n, k, 4000 + m + n + k)
+    got = gs.mx4_weight_dot(x.to(DEV), w, out_dtype=F32 if k % 2 else BF)
+    check_product(got, to_oracle(x), stored(w))
+
+
+@pytest.mark.parametrize("m,n,k", [(20, 3000, 8000), (50, 2000, 7001), (300, 1000, 200)])
+def test_weight_dot_reads_nothing_unwritten(m, n, k):
+    """A workspace full of NaN; x whose neighbours in memory are NaN; an x of infinities and NaN spoils its own rows only."""
+    x, _, w = operands(m, n, k, 51)
+    around = torch.full((m * k + 4096,), float("nan"), dtype=BF, device=DEV)
+    inner = around[2048:2048 + m * k].view(m, k)
+    inner.copy_(x)
+    ws = torch.full((1 << 25,), 255, dtype=torch.uint8, device=DEV)
+    got = gs.mx4_weight_dot(inner, w, workspace=ws)
+    check_product(got, to_oracle(x), stored(w))
+    inner[3, k - 1], inner[7, 0] = float("inf"), float("nan")
+    w.values[:, :, :] = torch.where(w.values == 0, 1, w.values)
+    again = gs.mx4_weight_dot(inner, w, act=gs.GS_ACT_NONE)
+    finite = torch.isfinite(again).all(1)
+    assert finite.sum() == m - 2 and not finite[3] and not finite[7]
 
 
 @pytest.mark.parametrize("odt", [BF, F32])
