@@ -107,7 +107,7 @@ struct AttendShape {
 };
 
 template <int D, int QT>
-__global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a) {
+__global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kernel(Mx4AttendArgs a) {
   using S = AttendShape<D, QT>;
   constexpr int C = S::C, KS = S::KS, VP = S::VP, kRows = S::kRows, kRow = S::kRow;
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -155,73 +155,84 @@ __global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a
       for (int j = 0; j < 8; ++j) o[t][p][j] = f32x4{0, 0, 0, 0};
   }
 
-  struct Tile {
-    uint32_t k[4][C], ks[4][KS], vs[4][VP];
-    i32x4 v[4][VP];
+  // Where the 4 runs of 16 tokens of a tile lie (wave-uniform).
+  struct Place {
+    const uint8_t* block[4];         // null: no page
+    uint32_t slot[4];
     int32_t token;
-    uint32_t there;                  // bit i: tokens 16 i .. of the tile are in a page
   };
   const int32_t* table = a.table + int64_t(b) * a.width;
-  auto page_of = [&](int32_t token, uint32_t* slot) -> int32_t {    // wave-uniform; below zero: none
-    if (token >= span.hi) return -1;
-    uint32_t entry;
-    a.cache.by_page.divmod(uint32_t(token), &entry, slot);
-    const int32_t id = table[entry];
-    return id < a.cache.n_pages ? id : -1;
-  };
-  auto load = [&](int32_t i, Tile& t) {
-    t.token = span.token(i);
-    t.there = 0;
+  auto find = [&](int32_t i) {
+    Place w;
+    w.token = span.token(i);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      uint32_t slot = 0;
-      const int32_t id = page_of(t.token + 16 * n, &slot);
-      if (id >= 0) {
-        t.there |= 1u << n;
-        const uint8_t* blk = a.cache.block(id, int(head));
-        load_dwords<C>(blk + slot * (D / 2) + uint32_t(r * (D / 2) + g * (D / 8)), t.k[n]);
-        const uint8_t* ks = blk + uint32_t(a.cache.page) * D + slot * C + uint32_t(r * C);
-        t.ks[n][0] = ks[(C * g) / 4];
-        if constexpr (KS == 2) t.ks[n][1] = ks[(C * g + C - 1) / 4];
+      const int32_t token = w.token + 16 * n;
+      w.block[n] = nullptr;
+      w.slot[n] = 0;
+      if (token < span.hi) {
+        uint32_t entry;
+        a.cache.by_page.divmod(uint32_t(token), &entry, &w.slot[n]);
+        const int32_t id = table[entry];
+        if (id >= 0 && id < a.cache.n_pages) w.block[n] = a.cache.block(id, int(head));
+      }
+    }
+    return w;
+  };
+  struct Keys {
+    uint32_t k[4][C], scale[4][KS];
+  };
+  struct Values {
+    i32x4 v[4][VP];
+    uint32_t scale[4][VP];
+  };
+  const uint32_t page = uint32_t(a.cache.page);
+  auto load_keys = [&](const Place& w, Keys& t) {
 #pragma unroll
-        for (int p = 0; p < VP; ++p) {
-          const int piece = 16 * p + r;
-          const bool ok = D / 8 - 16 * p >= 16 || piece < D / 8;
-          t.v[n][p] = i32x4{0, 0, 0, 0};
-          t.vs[n][p] = 0x7f7f7f7fu;
-          if (ok) {
-            t.v[n][p] = *reinterpret_cast<const i32x4*>(blk + uint32_t(a.cache.page) * (D / 2) + (slot / 4 + g) * (D * 2) + piece * 16);
-            t.vs[n][p] = *reinterpret_cast<const uint32_t*>(blk + uint32_t(a.cache.page) * (D + C) + ((slot / 4 + g) * C + piece / 4) * 4);
-          }
-        }
+    for (int n = 0; n < 4; ++n) {
+      if (w.block[n]) {
+        load_dwords<C>(w.block[n] + w.slot[n] * (D / 2) + uint32_t(r * (D / 2) + g * (D / 8)), t.k[n]);
+        const uint8_t* ks = w.block[n] + page * D + w.slot[n] * C + uint32_t(r * C);
+        t.scale[n][0] = ks[(C * g) / 4];
+        if constexpr (KS == 2) t.scale[n][1] = ks[(C * g + C - 1) / 4];
       } else {
 #pragma unroll
         for (int c = 0; c < C; ++c) t.k[n][c] = 0;
 #pragma unroll
-        for (int c = 0; c < KS; ++c) t.ks[n][c] = 127;
-#pragma unroll
-        for (int p = 0; p < VP; ++p) {
-          t.v[n][p] = i32x4{0, 0, 0, 0};
-          t.vs[n][p] = 0x7f7f7f7fu;
-        }
+        for (int c = 0; c < KS; ++c) t.scale[n][c] = 127;
       }
     }
+  };
+  auto load_values = [&](const Place& w, Values& t) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int p = 0; p < VP; ++p) {
+        const int piece = 16 * p + r;
+        t.v[n][p] = i32x4{0, 0, 0, 0};
+        t.scale[n][p] = 0x7f7f7f7fu;
+        if (w.block[n] && (D / 8 - 16 * p >= 16 || piece < D / 8)) {
+          t.v[n][p] = *reinterpret_cast<const i32x4*>(w.block[n] + page * (D / 2) + (w.slot[n] / 4 + g) * (D * 2) + piece * 16);
+          t.scale[n][p] = *reinterpret_cast<const uint32_t*>(w.block[n] + page * (D + C) + ((w.slot[n] / 4 + g) * C + piece / 4) * 4);
+        }
+      }
   };
   auto sees = [&](int32_t position, int32_t token) {
     return token <= position && (a.window == 0 || position - token < a.window || token < a.sinks);
   };
 
-  auto compute = [&](const Tile& t) {
+  // A tile: the next one's keys are requested once this one's are used up, and its values likewise, into the same registers.
+  auto compute = [&](const Place& at, const Place& next, bool more, Keys& keys, Values& t) {
     // scores: s[row tile][run of 16 tokens]
     f32x4 s[QT][4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       float sc[KS];
 #pragma unroll
-      for (int c = 0; c < KS; ++c) sc[c] = mx4_scale(t.ks[n][c]);
+      for (int c = 0; c < KS; ++c) sc[c] = mx4_scale(keys.scale[n][c]);
       i32x4 kv[C];
 #pragma unroll
-      for (int c = 0; c < C; ++c) kv[c] = mx4_decode8(t.k[n][c], KS == 1 || (C * g + c) / 4 == (C * g) / 4 ? sc[0] : sc[KS - 1]);
+      for (int c = 0; c < C; ++c) kv[c] = mx4_decode8(keys.k[n][c], KS == 1 || (C * g + c) / 4 == (C * g) / 4 ? sc[0] : sc[KS - 1]);
 #pragma unroll
       for (int u = 0; u < QT; ++u) {
         f32x4 acc = {0, 0, 0, 0};
@@ -230,9 +241,11 @@ __global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv[c]), __builtin_bit_cast(bf16x8, q[u][c]), acc, 0, 0, 0);
         s[u][n] = acc;
       }
+      __builtin_amdgcn_sched_barrier(0);               // (conversions ahead of their use cost registers)
     }
-    const bool all_seen = t.there == 15 && t.token + kTile - 1 <= pos_first &&
-                          (a.window == 0 || pos_last - t.token < a.window || t.token + kTile <= a.sinks);
+    if (more) load_keys(next, keys);
+    const bool all_seen = at.block[0] && at.block[1] && at.block[2] && at.block[3] && at.token + kTile - 1 <= pos_first &&
+                          (a.window == 0 || pos_last - at.token < a.window || at.token + kTile <= a.sinks);
     // weights, as the products with the values want them: p[row tile][half of the tile]
     i32x4 w[QT][2];
 #pragma unroll
@@ -247,7 +260,7 @@ __global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a
         for (int n = 0; n < 4; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!((t.there >> n) & 1) || !sees(pos[u], t.token + 16 * n + 4 * g + i)) e[4 * n + i] = -__builtin_inff();
+            if (!at.block[n] || !sees(pos[u], at.token + 16 * n + 4 * g + i)) e[4 * n + i] = -__builtin_inff();
       }
       float top = e[0];
 #pragma unroll
@@ -274,112 +287,111 @@ __global__ void __launch_bounds__(kWaves * 64) mx4_attend_kernel(Mx4AttendArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[u][h][i] = int32_t(pack_bf16x2(e[8 * h + 2 * i], e[8 * h + 2 * i + 1]));
     }
-    // scale bytes of 253 and more (2^126, 2^127, NaN) could make infinities or NaN of a number; times a weight of zero that would
-    // spoil rows that do not see the token
+    // Scale bytes of 253 and more (2^126, 2^127, NaN) could make infinities or NaN of numbers, and those times a weight of
+    // zero would spoil rows that do not see the token: their numbers are zero here and added one by one below.
     uint32_t wild = 0;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int p = 0; p < VP; ++p) wild |= ((t.vs[n][p] & 0x7f7f7f7fu) + 0x03030303u) & t.vs[n][p];
+      for (int p = 0; p < VP; ++p) wild |= ((t.scale[n][p] & 0x7f7f7f7fu) + 0x03030303u) & t.scale[n][p];
     const bool tame = !__any((wild & 0x80808080u) != 0);
-    auto values = [&](int h, int p, const float (&sc)[8], bool keep, i32x4 (&va)[8]) {
+    if (!tame) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {             // pairs of tokens of one run of 16
-        const i32x4 raw = t.v[2 * h + half][p];
-        uint32_t d[4][4];                                // [token][pair of numbers]
+      for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t x = keep ? uint32_t(raw[j]) : 0u;
-          const i32x4 y = mx4_decode8(x, sc[4 * half + j]);
+        for (int p = 0; p < VP; ++p)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) d[j][c] = uint32_t(y[c]);
+          for (int j = 0; j < 4; ++j)
+            if (((t.scale[n][p] >> (8 * j)) & 255u) >= 253u) {
+              t.v[n][p][j] = 0;
+              t.scale[n][p] = (t.scale[n][p] & ~(255u << (8 * j))) | 127u << (8 * j);
+            }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int p = 0; p < VP; ++p) {
+        i32x4 va[8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {           // pairs of tokens of one run of 16
+          uint32_t d[4][4];                              // [token][pair of numbers]
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t x = ((t.scale[2 * h + half][p] >> (8 * j)) & 255u) << 23;
+            const i32x4 y = mx4_decode8(uint32_t(t.v[2 * h + half][p][j]), __uint_as_float(x > 0x00400000u ? x : 0x00400000u));
+#pragma unroll
+            for (int c = 0; c < 4; ++c) d[j][c] = uint32_t(y[c]);
+          }
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              va[2 * c][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x05040100u));
+              va[2 * c + 1][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x07060302u));
+            }
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            va[2 * c][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x05040100u));
-            va[2 * c + 1][2 * half + j] = int32_t(__builtin_amdgcn_perm(d[2 * j + 1][c], d[2 * j][c], 0x07060302u));
-          }
-      }
-    };
-    if (tame) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int p = 0; p < VP; ++p) {
-          float sc[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint32_t x = ((t.vs[2 * h + j / 4][p] >> (8 * (j % 4))) & 255u) << 23;
-            sc[j] = __uint_as_float(x > 0x00400000u ? x : 0x00400000u);
-          }
-          i32x4 va[8];
-          values(h, p, sc, true, va);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int u = 0; u < QT; ++u)
-              o[u][p][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[j]), __builtin_bit_cast(bf16x8, w[u][h]),
-                                                                   o[u][p][j], 0, 0, 0);
-        }
-    } else {
-      // block by block of 32 numbers: the scales go to the weights of the tokens that a row sees
-      const float one[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-#pragma unroll 1
-      for (int blk = 0; blk < C; ++blk) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t bytes[2];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t slot = 0;
-            const int32_t id = page_of(t.token + 16 * (2 * h + half), &slot);
-            bytes[half] = 0x7f7f7f7fu;
-            if (id >= 0)
-              bytes[half] = *reinterpret_cast<const uint32_t*>(a.cache.block(id, int(head)) + uint32_t(a.cache.page) * (D + C) +
-                                                               ((slot / 4 + g) * C + blk) * 4);
-          }
-          i32x4 scaled[QT];
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
           for (int u = 0; u < QT; ++u)
+            o[u][p][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[j]), __builtin_bit_cast(bf16x8, w[u][h]),
+                                                                 o[u][p][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    if (!tame) {
+#pragma unroll 1
+      for (int32_t token = at.token; token < at.token + kTile && token < span.hi; ++token) {
+        uint32_t entry, slot;
+        a.cache.by_page.divmod(uint32_t(token), &entry, &slot);
+        const int32_t id = table[entry];
+        if (id < 0 || id >= a.cache.n_pages) continue;
+        const uint8_t* blk = a.cache.block(id, int(head));
+        const int32_t of = token - at.token, mine = of / 16 * 4 + of % 4;     // which of a lane's 16 weights, in lanes of group of / 4 % 4
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+          float weight = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t x = uint32_t(w[u][i / 8][i / 2 % 4]);
+            weight = i == mine ? __uint_as_float(i % 2 ? x & 0xffff0000u : x << 16) : weight;
+          }
+          weight = __shfl(weight, of / 4 % 4 * 16 + r);
+#pragma unroll
+          for (int p = 0; p < VP; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              float f[2];
+              const int piece = 16 * p + 4 * g + i;      // the pieces that the lane has results of
+              if (piece >= D / 8 || !sees(pos[u], token)) continue;
+              const uint32_t byte = blk[page * (D + C) + (slot / 4 * C + piece / 4) * 4 + slot % 4];
+              if (byte < 253) continue;
+              const uint32_t x = *reinterpret_cast<const uint32_t*>(blk + page * (D / 2) + ((slot / 4 * (D / 8) + piece) * 4 + slot % 4) * 4);
+              const float scaled = weight * mx4_scale(byte);
+              float f[8];
+              mx4_decode2_f32<0>(x, 1.0f, f);
+              mx4_decode2_f32<1>(x, 1.0f, f + 2);
+              mx4_decode2_f32<2>(x, 1.0f, f + 4);
+              mx4_decode2_f32<3>(x, 1.0f, f + 6);
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int n = 2 * h + i / 2, j = 2 * (i % 2) + k;      // run of 16, token of the lane's four
-                const float weight = __uint_as_float(k ? uint32_t(w[u][h][i]) & 0xffff0000u : uint32_t(w[u][h][i]) << 16);
-                const bool seen = ((t.there >> n) & 1) && sees(pos[u], t.token + 16 * n + 4 * g + j);
-                f[k] = seen ? weight * mx4_scale((bytes[i / 2] >> (8 * j)) & 255u) : 0.0f;
-              }
-              scaled[u][i] = int32_t(pack_bf16x2(f[0], f[1]));
+              for (int j = 0; j < 8; ++j) o[u][p][j][i] += scaled * f[j];
             }
-#pragma unroll
-          for (int p = 0; p < VP; ++p) {
-            i32x4 va[8];
-            values(h, p, one, (16 * p + r) / 4 == blk, va);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-              for (int u = 0; u < QT; ++u) {
-                const f32x4 add = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[j]), __builtin_bit_cast(bf16x8, scaled[u]),
-                                                                          f32x4{0, 0, 0, 0}, 0, 0, 0);
-                // lane (r, g) receives piece 16 p + 4 g + i: only those of this block (others are zero, or NaN)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if ((16 * p + 4 * g + i) / 4 == blk) o[u][p][j][i] += add[i];
-              }
-          }
         }
       }
     }
   };
 
-  for (int32_t i = begin + wave; i < stop; i += kWaves) {
-    Tile t;
-    load(i, t);
-    compute(t);
+  if (begin + wave < stop) {
+    Keys keys;
+    Values values;
+    Place at = find(begin + wave);
+    load_keys(at, keys);
+    load_values(at, values);
+    for (int32_t i = begin + wave; i < stop; i += kWaves) {
+      const bool more = i + kWaves < stop;
+      const Place next = more ? find(i + kWaves) : at;
+      compute(at, next, more, keys, values);
+      if (more) load_values(next, values);
+      at = next;
+    }
   }
 
   // join the waves, 16 rows at a time
