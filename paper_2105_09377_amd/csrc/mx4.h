@@ -130,7 +130,8 @@ struct Mx4AttendArgs {
   int64_t window, sinks;  // window 0: everything
   int64_t batch, width;
   int32_t queries, group;
-  int32_t parts, tiles;   // set by the launcher: workgroups along a sequence; 16-row tiles of a workgroup
+  int32_t parts, tiles;   // set by the launcher: workgroups along a sequence; 16-row tiles of a workgroup;
+  int32_t least;          // 64-token tiles of a part
 };
 hipError_t launch_mx4_attend(const Mx4AttendArgs& a, hipStream_t s);
 size_t mx4_attend_workspace(const Mx4AttendArgs& a);

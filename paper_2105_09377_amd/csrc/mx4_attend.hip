@@ -11,47 +11,14 @@
 //     weights a lane already has: it reads piece r of those 4 tokens (16 bytes), converts, and pairs tokens by byte permutation.
 //     Lane (r, g) receives numbers 8 (4 g + i) + j of row r.
 // So a row's maximum, sum and correction are one register, the same for all of a lane's scores and results.
-#include "mx4.h"
+// Many rows have a kernel of their own (mx4_attend_many.h).
+#include "mx4_attend_many.h"
 
 namespace gs {
 
 namespace {
 
-constexpr int kTile = 64;            // tokens of a wave's step
 constexpr int kWaves = 4;
-constexpr int kMinTiles = 8;         // of a part: two per wave
-constexpr int kMaxParts = 64;        // the joining kernel has a lane for each
-// Weights are 2^(score - maximum - kHeadroom): their sum over 2^24 tokens, times the largest number of the format, does not
-// overflow before it is divided by their sum.
-constexpr float kHeadroom = 24.0f;
-
-// What the rows row0 .. row1 of a sequence of `len` tokens have to look at, in tiles: the first `sink_tiles`, then
-// those from `window_tile` on.  Cut into parts of `per` tiles.
-struct Span {
-  int32_t hi;                        // tokens from here on are seen by no row
-  int32_t sink_tiles, window_tile, total, per, parts;
-  __device__ int32_t token(int32_t i) const { return (i < sink_tiles ? i : window_tile + i - sink_tiles) * kTile; }
-};
-__device__ __forceinline__ Span span_of(const Mx4AttendArgs& a, int32_t len, int32_t row0, int32_t row1) {
-  Span s;
-  const int32_t first = len - a.queries + row0 / a.group, last = len - a.queries + row1 / a.group;    // positions
-  s.hi = last + 1 > 0 ? last + 1 : 0;
-  int32_t lo = 0;
-  if (a.window > 0 && first >= a.window) lo = first - int32_t(a.window) + 1;
-  const int32_t sinks = a.sinks < lo ? int32_t(a.sinks) : lo;
-  s.sink_tiles = (sinks + kTile - 1) / kTile;
-  s.window_tile = lo / kTile > s.sink_tiles ? lo / kTile : s.sink_tiles;
-  const int32_t end = (s.hi + kTile - 1) / kTile;
-  s.total = s.sink_tiles + (end > s.window_tile ? end - s.window_tile : 0);
-  s.per = (s.total + a.parts - 1) / a.parts;
-  s.per = s.per > kMinTiles ? s.per : kMinTiles;
-  s.parts = s.total > s.per ? (s.total + s.per - 1) / s.per : 1;
-  return s;
-}
-__device__ __forceinline__ int32_t length_of(const Mx4AttendArgs& a, int64_t b) {
-  const int32_t len = a.lengths[b], most = int32_t(a.width) * a.cache.page;
-  return len < 0 ? 0 : len < most ? len : most;
-}
 
 // Maximum and sum over the four lanes that have the same r.
 __device__ __forceinline__ float max_over_g(float v) {
@@ -70,8 +37,6 @@ __device__ __forceinline__ float sum_over_g(float v) {
   p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // N dwords from an address aligned to 4 bytes (8 where N is even, 16 where it is a multiple of 4).
 template <int N>
@@ -515,15 +480,17 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
 // Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
 void plan(Mx4AttendArgs* a) {
   const int64_t rows = int64_t(a->queries) * a->group;
-  a->tiles = rows > 16 ? 2 : 1;
+  a->tiles = rows > 32 ? 8 : rows > 16 ? 2 : 1;
+  a->least = a->tiles == 8 ? 4 : 8;
   const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles);
   int64_t most = a->width * a->cache.page;
   if (a->window > 0) {
     const int64_t seen = a->window + a->queries + (a->sinks < most ? a->sinks : most) + 2 * kTile;
     most = seen < most ? seen : most;
   }
-  int64_t parts = ceil_div(1024, tasks > 0 ? tasks : 1);
-  const int64_t useful = ceil_div(ceil_div(most, kTile), kMinTiles);
+  const int64_t some = tasks > 0 ? tasks : 1;
+  int64_t parts = a->tiles == 8 ? (512 + some / 2) / some : ceil_div(1024, some);
+  const int64_t useful = ceil_div(ceil_div(most, kTile), a->least);
   parts = parts < useful ? parts : useful;
   parts = parts < kMaxParts ? parts : kMaxParts;
   a->parts = int32_t(parts > 1 ? parts : 1);
@@ -531,15 +498,24 @@ void plan(Mx4AttendArgs* a) {
 
 template <int D, int QT>
 hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
-  using S = AttendShape<D, QT>;
+  constexpr bool kMany = QT == 8;
+  constexpr int kRows = 16 * QT;
   const int64_t rows = int64_t(a.queries) * a.group;
-  const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, S::kRows) * a.parts;
+  const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, kRows) * a.parts;
   const int64_t total_rows = a.batch * a.cache.heads * rows;
   if (groups > 0x7fffffff || total_rows > 0x7fffffff) return hipErrorInvalidValue;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(mx4_attend_kernel<D, QT>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, int(S::kLds));
+  void (*kernel)(Mx4AttendArgs);
+  size_t lds;
+  if constexpr (kMany) {
+    kernel = mx4_attend_many_kernel<D>;
+    lds = ManyShape<D>::kLds;
+  } else {
+    kernel = mx4_attend_kernel<D, QT>;
+    lds = AttendShape<D, QT>::kLds;
+  }
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((mx4_attend_kernel<D, QT>), dim3(unsigned(groups)), dim3(kWaves * 64), S::kLds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kWaves * 64), lds, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     hipLaunchKernelGGL((mx4_attend_join_kernel<D, QT>), dim3(unsigned(ceil_div(total_rows, 4))), dim3(256), 0, s, a, total_rows);
@@ -549,7 +525,7 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
 }
 template <int D>
 hipError_t launch_d(const Mx4AttendArgs& a, hipStream_t s) {
-  return a.tiles == 1 ? launch<D, 1>(a, s) : launch<D, 2>(a, s);
+  return a.tiles == 1 ? launch<D, 1>(a, s) : a.tiles == 2 ? launch<D, 2>(a, s) : launch<D, 8>(a, s);
 }
 
 }  // namespace

@@ -1,0 +1,345 @@
+// Attention over the 4-bit cache for many rows: prompts, and chunks of them over what was cached before.
+//
+// A workgroup has 128 rows, 32 per wave, that share a cache head, and walks the tokens in tiles of 64 that all of its waves use: the
+// tile's codes are converted to bfloat16 once (exactly) into LDS, the next tile's while this one is multiplied, the one
+// behind that on its way into registers.  With r = lane % 32, h = lane / 32 (32x32x16 bfloat16):
+//   scores: 32 tokens x 32 rows per product.  Keys lie in LDS as they are, token after token.  Lane (r, h) receives the scores of
+//     row r with tokens 8 (v / 4) + 4 h + v % 4.
+//   output: 32 numbers x 32 rows per product, over 16 tokens whose weights a lane already has: values lie in LDS one row of 64 tokens per
+//     number, the tokens of each 16 in the order 0..3, 8..11, 4..7, 12..15, so that a lane's eight are 16 bytes.
+// Rows in LDS are an odd multiple of 16 bytes long: reads and writes of 16 rows fall on different banks.
+#pragma once
+
+#include "mx4_span.h"
+
+namespace gs {
+
+namespace {
+
+template <int D>
+struct ManyShape {
+  static constexpr int NB = D / 32;                      // blocks of a token; 64 units of 16 bytes of a tile's keys each, and of its values
+  static constexpr int U = (2 * NB + 3) / 4;             // units of a lane
+  static constexpr int kKeyRow = 2 * D + 16, kValueRow = 2 * kTile + 16;
+  static constexpr int kBuf = kTile * kKeyRow + D * kValueRow;
+  static constexpr int kMeta = 16;                       // bytes: 0-3 whether a run of 16 tokens has a page, 4-11 scales of 2^126 and more
+  static constexpr int kRows = 128;
+  static constexpr size_t kLds = 2 * (kBuf + kMeta);
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(Mx4AttendArgs a) {
+  using S = ManyShape<D>;
+  constexpr int NB = S::NB, U = S::U, kRows = S::kRows, kKeyRow = S::kKeyRow, kValueRow = S::kValueRow;
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds_many[];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+  const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
+  // each XCD (every eighth workgroup) gets consecutive tasks: row tiles of one cache head read the same pages
+  const uint32_t per = gridDim.x / 8, rem = gridDim.x % 8, xcd = blockIdx.x % 8;
+  uint32_t at = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
+  const uint32_t part = at % uint32_t(a.parts);
+  at /= uint32_t(a.parts);
+  const uint32_t row_tile = at % uint32_t(row_tiles), bh = at / uint32_t(row_tiles);
+  const uint32_t b = bh / uint32_t(a.cache.heads), head = bh - b * uint32_t(a.cache.heads);
+  const int32_t row0 = int32_t(row_tile) * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
+  const int32_t len = length_of(a, b);
+  const Span span = span_of(a, len, row0, row1);
+  if (int32_t(part) >= span.parts) return;
+  const int32_t begin = int32_t(part) * span.per, stop = begin + span.per < span.total ? begin + span.per : span.total;
+
+  // the wave's rows
+  const int32_t first_row = row0 + wave * 32, last_row = first_row + 31 < rows ? first_row + 31 : rows - 1;
+  const bool active = first_row < rows;
+  const int32_t pos_first = len - a.queries + first_row / a.group, pos_last = len - a.queries + last_row / a.group;
+  const int32_t row = first_row + r, qi = row / a.group, qh = row - qi * a.group;
+  const int32_t pos = row < rows ? len - a.queries + qi : -1;
+  const int64_t row_at = ((int64_t(b) * a.queries + qi) * a.cache.heads + head) * a.group * D + int64_t(qh) * D;
+  // a negative scale turns the signs of the queries, so that the largest score is the largest product
+  const uint32_t turn = a.scale < 0 ? 0x80008000u : 0u;
+  const float to_log2 = fabsf(a.scale) * 1.44269504088896340736f;
+  i32x4 q[2 * NB];
+#pragma unroll
+  for (int s = 0; s < 2 * NB; ++s) {
+    q[s] = i32x4{0, 0, 0, 0};
+    if (row < rows) q[s] = *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(a.q) + row_at + s * 16 + h * 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[s][i] ^= int32_t(turn);
+  }
+
+  f32x16 o[NB];
+  float m = -__builtin_inff(), l = 0;
+#pragma unroll
+  for (int d = 0; d < NB; ++d)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[d][v] = 0;
+
+  // A lane's units of a tile: a block of a token's key, or 8 numbers of 4 tokens' values.  The first NB of the wave's share are keys.
+  const int32_t* const table = a.table + int64_t(b) * a.width;
+  const uint32_t page = uint32_t(a.cache.page);
+  int32_t ids[U];
+  uint32_t have = 0;                                     // units of `raw` whose token has a page
+  i32x4 raw[U];
+  uint32_t raw_scale[U];
+  auto key_unit = [&](int u) { return wave + 4 * u < NB; };
+  auto value_unit = [&](int u) { return wave + 4 * u >= NB && wave + 4 * u < 2 * NB; };
+  auto lane_of = [&](int u) { return (wave + 4 * u < NB ? wave + 4 * u : wave + 4 * u - NB) * 64 + lane; };
+  auto token_of = [&](int u) { return key_unit(u) ? lane_of(u) / NB : lane_of(u) % 16 * 4; };
+  auto find = [&](int32_t i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      ids[u] = -1;
+      const int32_t token = span.token(i) + token_of(u);
+      if (i < stop && wave + 4 * u < 2 * NB && token < span.hi) {
+        uint32_t entry, slot;
+        a.cache.by_page.divmod(uint32_t(token), &entry, &slot);
+        ids[u] = table[entry];
+      }
+    }
+  };
+  auto load = [&](int32_t i) {
+    have = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (ids[u] < 0 || ids[u] >= a.cache.n_pages) {
+        raw[u] = i32x4{0, 0, 0, 0};
+        raw_scale[u] = 0x7f7f7f7fu;
+        continue;
+      }
+      have |= 1u << u;
+      uint32_t entry, slot;
+      a.cache.by_page.divmod(uint32_t(span.token(i) + token_of(u)), &entry, &slot);
+      const uint8_t* const block = a.cache.block(ids[u], int(head));
+      const uint32_t of = uint32_t(lane_of(u));
+      if (key_unit(u)) {
+        raw[u] = *reinterpret_cast<const i32x4*>(block + slot * (D / 2) + of % NB * 16);
+        raw_scale[u] = block[page * D + slot * NB + of % NB];
+      } else {
+        raw[u] = *reinterpret_cast<const i32x4*>(block + page * (D / 2) + slot * (D / 2) + of / 16 * 16);
+        raw_scale[u] = *reinterpret_cast<const uint32_t*>(block + page * (D + NB) + slot * NB + of / 64 * 4);
+      }
+    }
+  };
+  auto convert = [&](uint8_t* buf) {
+    uint8_t* const meta = buf + S::kBuf;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (key_unit(u)) {
+        const int token = lane_of(u) / NB, block = lane_of(u) % NB;
+        uint8_t* const dst = buf + token * kKeyRow + block * 64;
+        const float s = mx4_scale(raw_scale[u]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *reinterpret_cast<i32x4*>(dst + 16 * c) = mx4_decode8(uint32_t(raw[u][c]), s);
+        if (block == 0 && token % 16 == 0) meta[token / 16] = uint8_t((have >> u) & 1u);
+      } else if (value_unit(u)) {
+        // Scale bytes of 253 and more could make infinities or NaN of numbers, and those times a weight of zero would spoil rows
+        // that do not see the token: their numbers are zero here and added one by one below.
+        const bool wild = ((((raw_scale[u] & 0x7f7f7f7fu) + 0x03030303u) & raw_scale[u]) & 0x80808080u) != 0;
+        if (__any(wild)) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (((raw_scale[u] >> (8 * j)) & 255u) >= 253u) raw[u][j] = 0;
+          if (lane == 0) meta[4 + wave + 4 * u - NB] = 1;
+        } else if (lane == 0) {
+          meta[4 + wave + 4 * u - NB] = 0;
+        }
+        uint32_t d[4][4];                                // [token][pair of numbers]
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t byte = (raw_scale[u] >> (8 * j)) & 255u, x = byte < 253 ? byte << 23 : 0u;
+          const i32x4 y = mx4_decode8(uint32_t(raw[u][j]), __uint_as_float(x > 0x00400000u ? x : 0x00400000u));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) d[j][c] = uint32_t(y[c]);
+        }
+        const int four = lane_of(u) % 16, piece = lane_of(u) / 16;
+        uint8_t* const dst = buf + kTile * kKeyRow + piece * 8 * kValueRow + four / 4 * 32 + four % 2 * 16 + four / 2 % 2 * 8;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int odd = 0; odd < 2; ++odd) {
+            const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+            *reinterpret_cast<i32x2*>(dst + (2 * c + odd) * kValueRow) =
+                i32x2{int32_t(__builtin_amdgcn_perm(d[1][c], d[0][c], sel)), int32_t(__builtin_amdgcn_perm(d[3][c], d[2][c], sel))};
+          }
+      }
+    }
+  };
+  const int32_t window = a.window > 0 ? int32_t(a.window) : 0x7fffffff, sinks = int32_t(a.sinks);
+  auto sees = [&](int32_t position, int32_t token) {
+    return token <= position && (position - token < window || token < sinks);
+  };
+
+  auto compute = [&](const uint8_t* buf, int32_t token0) {
+    const i32x4 meta = *reinterpret_cast<const i32x4*>(buf + S::kBuf);
+    const uint32_t pages = __builtin_amdgcn_readfirstlane(meta[0]);
+    const bool tame = __builtin_amdgcn_readfirstlane(meta[1] | meta[2]) == 0;
+    f32x16 s[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[n][v] = 0;
+#pragma unroll
+      for (int c = 0; c < 2 * NB; ++c) {
+        const i32x4 k = *reinterpret_cast<const i32x4*>(buf + (n * 32 + r) * kKeyRow + c * 32 + h * 16);
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s[n], 0, 0, 0);
+      }
+    }
+    const bool all_seen = pages == 0x01010101u && token0 + kTile - 1 <= pos_first &&
+                          (pos_last - token0 < window || token0 + kTile <= sinks);
+    uint32_t seen = ~0u;                                 // bit 16 n + v
+    if (!all_seen) {
+      seen = 0;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int of = 32 * n + 8 * (v / 4) + v % 4;
+          const bool ok = ((pages >> (of / 16 * 8)) & 1u) && sees(pos, token0 + of + 4 * h);
+          seen |= uint32_t(ok) << (16 * n + v);
+        }
+    }
+    float top = -__builtin_inff();
+    if (all_seen) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
+    } else {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, (seen >> (16 * n + v)) & 1u ? s[n][v] : -__builtin_inff());
+    }
+    const uint32_t bits = __float_as_uint(top);
+    const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    top = top == -__builtin_inff() ? m : fmaxf(top * to_log2 + kHeadroom, m);      // (a scale of 0 times -infinity is no maximum)
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    if (__any(top > m)) {
+      const float shrink = exp2_fast(m - ref);
+      m = top;
+      l *= shrink;
+#pragma unroll
+      for (int d = 0; d < NB; ++d)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[d][v] *= shrink;
+    }
+    i32x4 w[2][2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[n][v] = exp2_fast(fmaf(s[n][v], to_log2, -ref));
+      if (!all_seen)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[n][v] = (seen >> (16 * n + v)) & 1u ? s[n][v] : 0.0f;
+      float sum[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum[v % 4] += s[n][v];
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) w[n][v / 8][v / 2 % 4] = int32_t(pack_bf16x2(s[n][v], s[n][v + 1]));
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int d = 0; d < NB; ++d) {
+          const i32x4 x = *reinterpret_cast<const i32x4*>(buf + kTile * kKeyRow + (d * 32 + r) * kValueRow + (2 * n + c) * 32 + h * 16);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w[n][c]), o[d], 0, 0, 0);
+        }
+    if (!tame) {
+#pragma unroll 1
+      for (int32_t token = token0; token < token0 + kTile && token < span.hi; ++token) {
+        uint32_t entry, slot;
+        a.cache.by_page.divmod(uint32_t(token), &entry, &slot);
+        const int32_t id = table[entry];
+        if (id < 0 || id >= a.cache.n_pages) continue;
+        const uint8_t* const block = a.cache.block(id, int(head));
+        const int32_t of = token - token0, mine = of / 8 * 4 + of % 4;       // which of a lane's 32 weights, in lanes of half of / 4 % 2
+        float weight = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const uint32_t x = uint32_t(w[i / 16][i / 8 % 2][i / 2 % 4]);
+          weight = i == mine ? __uint_as_float(i % 2 ? x & 0xffff0000u : x << 16) : weight;
+        }
+        weight = __shfl(weight, of / 4 % 2 * 32 + r);
+        if (!sees(pos, token)) continue;
+#pragma unroll
+        for (int d = 0; d < NB; ++d) {
+          const uint32_t byte = block[page * (D + NB) + (slot / 4 * NB + d) * 4 + slot % 4];
+          if (byte < 253) continue;
+          const float scaled = weight * mx4_scale(byte);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {                  // numbers 8 g + 4 h .. of the block
+            const uint32_t x = reinterpret_cast<const uint16_t*>(block + page * (D / 2) + ((slot / 4 * (D / 8) + 4 * d + g) * 4 + slot % 4) * 4)[h];
+            float f[4];
+            mx4_decode2_f32<0>(x, 1.0f, f);
+            mx4_decode2_f32<1>(x, 1.0f, f + 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[d][4 * g + j] += scaled * f[j];
+          }
+        }
+      }
+    }
+  };
+
+  if (threadIdx.x < 2) *reinterpret_cast<i32x4*>(lds_many + threadIdx.x * (S::kBuf + S::kMeta) + S::kBuf) = i32x4{0, 0, 0, 0};
+  __syncthreads();
+  if (begin < stop) {
+    find(begin);
+    load(begin);
+    convert(lds_many);
+    find(begin + 1);
+    load(begin + 1);
+    find(begin + 2);
+    __syncthreads();
+    int buf = 0;
+    for (int32_t i = begin; i < stop; ++i) {
+      if (i + 1 < stop) {
+        convert(lds_many + (buf ^ 1) * (S::kBuf + S::kMeta));
+        load(i + 2);
+        find(i + 3);
+      }
+      const int32_t token0 = span.token(i);
+      const bool any_seen = active && token0 <= pos_last &&
+                            (pos_first - (token0 + kTile - 1) < window || token0 < sinks);
+      if (any_seen) compute(lds_many + buf * (S::kBuf + S::kMeta), token0);
+      __syncthreads();
+      buf ^= 1;
+    }
+  }
+
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  const float total = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+  if (row >= rows) return;
+  if (span.parts == 1) {
+    const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float x0 = o[d][4 * g] * inv, x1 = o[d][4 * g + 1] * inv, x2 = o[d][4 * g + 2] * inv, x3 = o[d][4 * g + 3] * inv;
+        const int64_t dst = row_at + d * 32 + g * 8 + h * 4;
+        if (a.out_dtype == GS_BF16)
+          *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + dst) = i32x2{int32_t(pack_bf16x2(x0, x1)), int32_t(pack_bf16x2(x2, x3))};
+        else
+          *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + dst) = f32x4{x0, x1, x2, x3};
+      }
+  } else {
+    const int64_t task = int64_t(bh) * row_tiles + row_tile;
+    float* const dst = a.partial + ((task * a.parts + part) * kRows + wave * 32 + r) * (D + 2);
+    if (h == 0) *reinterpret_cast<f32x2_t*>(dst) = f32x2_t{m, total};
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2)
+          *reinterpret_cast<f32x2_t*>(dst + 2 + d * 32 + g * 8 + h * 4 + j) = f32x2_t{o[d][4 * g + j], o[d][4 * g + j + 1]};
+  }
+}
+
+}  // namespace
+
+}  // namespace gs

@@ -347,6 +347,47 @@ def test_attend_windows(queries, dim, page, window, sinks):
     check_attention(q, cache, table, torch.tensor([300, 200], dtype=torch.int32), dim ** -0.5, window=window, sinks=sinks)
 
 
+MANY_ROWS = [  # more than 32 rows of a cache head: tiles of 128 rows, the last of them partly empty
+    (1, 33, 1, 1, 64, 16, 33), (2, 100, 2, 4, 64, 16, 400), (1, 129, 1, 1, 128, 32, 200), (2, 64, 1, 3, 96, 16, 1000), (1, 50, 2, 2, 192, 48, 700),
+    (1, 70, 1, 2, 256, 16, 600), (3, 130, 1, 1, 64, 64, 1500), (1, 40, 1, 1, 128, 16, 3000), (1, 9, 2, 16, 256, 64, 1300), (2, 257, 1, 1, 96, 128, 257)]
+
+
+@pytest.mark.parametrize("batch,queries,heads,group,dim,page,longest", MANY_ROWS)
+def test_attend_many_rows(batch, queries, heads, group, dim, page, longest):
+    seed = 700 + longest + dim
+    cache, table = filled_cache(batch, longest, heads, dim, page, seed)
+    q = normal((batch, queries, heads * group, dim), seed + 5)
+    lengths = torch.tensor([max(queries - 3 * b, longest - 50 * b) for b in range(batch)], dtype=torch.int32)
+    check_attention(q, cache, table, lengths, dim ** -0.5, odt=BF if dim == 96 else F32)
+
+
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (77, 4), (200, 130), (0, 0)])
+def test_attend_many_rows_in_windows(dim, window, sinks):
+    cache, table = filled_cache(2, 500, 1, dim, 16, 710 + dim)
+    table[1, 7], table[1, 20] = -1, 10**6
+    q = normal((2, 60, 3, dim), 711)
+    check_attention(q, cache, table, torch.tensor([500, 433], dtype=torch.int32), dim ** -0.5, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dim", [64, 192])
+@pytest.mark.parametrize("scale", [0.1, -0.3, 0.0])
+def test_attend_many_rows_odd_numbers(dim, scale):
+    """Wide and NaN value scales that some rows see; negative and zero scales; query rows of infinities and NaN."""
+    page, n = 16, 300
+    cache, table = filled_cache(1, n, 1, dim, page, 720)
+    for t, blk, byte in ((230, 1, 255), (275, 0, 254), (40, 0, 253), (290, 1, 253)):
+        off = mx4.token_offsets(page, dim, t % page)[3][blk]
+        cache.data[int(table[0, t // page]), 0, off] = byte
+    q = normal((1, 100, 1, dim), 721) * 0.3
+    check_attention(q, cache, table, torch.tensor([n], dtype=torch.int32), scale, window=150)
+    clean = gs.mx4_attend(q.to(DEV), cache, table.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), 0.1, window=20)
+    q[0, 3, 0, 5], q[0, 50, 0, 0] = float("inf"), float("nan")
+    got = gs.mx4_attend(q.to(DEV), cache, table.to(DEV), torch.tensor([n], dtype=torch.int32, device=DEV), 0.1, window=20)
+    keep = [i for i in range(100) if i not in (3, 50)]
+    assert torch.equal(torch.nan_to_num(got[0, keep]), torch.nan_to_num(clean[0, keep])) and torch.isnan(got[0, 50]).all()
+
+
 def test_attend_long_window_in_parts():
     cache, table = filled_cache(1, 4000, 1, 64, 64, 420)
     q = normal((1, 2, 2, 64), 421)
