@@ -86,38 +86,93 @@ __device__ __forceinline__ uint32_t block_scale_byte(const float (&x)[8]) {
   return mx4_scale_byte(max_of_4_lanes(top));
 }
 
-// A row's pieces of 8 numbers are counted up to whole runs of scale bytes (`per_row`, a multiple of 32), the padding
-// written as zeros by the same lanes.
-template <int DT>
-__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a, int64_t per_row, int64_t total) {
-  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols);
-  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
-    const int64_t row = at / per_row, piece = at - row * per_row;
-    float x[8];
-    const void* src = static_cast<const uint8_t*>(a.plain) + row * a.cols * int64_t(dtype_size(DT));
-    load8<DT>(src, piece * 8, a.cols - piece * 8, x);
-    const uint32_t byte = block_scale_byte(x);
-    const int64_t block = piece / 4;
-    if (block < blocks) static_cast<uint32_t*>(a.values)[row * blocks * 4 + piece] = mx4_encode8(x, byte);
-    if (piece % 4 == 0) static_cast<uint8_t*>(a.scales)[row * pitch + block] = uint8_t(block < blocks ? byte : 0);
+// Pieces of 8 numbers of all rows, one after the other: a workgroup takes 256 P of them, a lane P that lie 256 apart, whose loads are
+// all under way before the first is used.  Rows and places in them come from a division by multiplication where all pieces count in 32
+// bits (BIG: 64-bit divisions).
+template <bool BIG>
+struct Pieces {
+  int64_t per_row, total;
+  FastDiv by_row;
+  __device__ void place(int64_t at, int64_t* row, int64_t* piece) const {
+    if constexpr (BIG) {
+      *row = at / per_row;
+      *piece = at - *row * per_row;
+    } else {
+      uint32_t q, r;
+      by_row.divmod(uint32_t(at), &q, &r);
+      *row = q;
+      *piece = r;
+    }
+  }
+};
+
+// A row's pieces are counted up to whole runs of scale bytes (a multiple of 32), the padding written as zeros by the same lanes.
+template <int DT, int P, bool BIG>
+__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
+  int64_t row[P], piece[P];
+  float x[P][8];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t at = base + p * kThreads;
+    const bool there = at < n.total;
+    n.place(there ? at : 0, &row[p], &piece[p]);
+    if (!there) row[p] = -1;
+    const void* const src = static_cast<const uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
+    load8<DT>(src, piece[p] * 8, there ? a.cols - piece[p] * 8 : 0, x[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const uint32_t byte = block_scale_byte(x[p]);
+    if (row[p] < 0) continue;
+    const int64_t block = piece[p] / 4;
+    if (block < blocks) static_cast<uint32_t*>(a.values)[row[p] * blocks * 4 + piece[p]] = mx4_encode8(x[p], byte);
+    if (piece[p] % 4 == 0) static_cast<uint8_t*>(a.scales)[row[p] * pitch + block] = uint8_t(block < blocks ? byte : 0);
   }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs a, int64_t per_row, int64_t total) {
-  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols);
-  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
-    const int64_t row = at / per_row, piece = at - row * per_row;
-    const uint32_t w = static_cast<const uint32_t*>(a.values)[row * blocks * 4 + piece];
-    const uint32_t byte = static_cast<const uint8_t*>(a.scales)[row * pitch + piece / 4];
-    void* dst = static_cast<uint8_t*>(a.plain) + row * a.cols * int64_t(dtype_size(DT));
-    store8<DT>(dst, piece * 8, a.cols - piece * 8, w, mx4_scale(byte));
+template <int DT, int P, bool BIG>
+__global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
+  int64_t row[P], piece[P];
+  uint32_t w[P], byte[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t at = base + p * kThreads;
+    n.place(at < n.total ? at : 0, &row[p], &piece[p]);
+    w[p] = static_cast<const uint32_t*>(a.values)[row[p] * blocks * 4 + piece[p]];
+    byte[p] = static_cast<const uint8_t*>(a.scales)[row[p] * pitch + piece[p] / 4];
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (base + p * kThreads >= n.total) continue;
+    void* const dst = static_cast<uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
+    store8<DT>(dst, piece[p] * 8, a.cols - piece[p] * 8, w[p], mx4_scale(byte[p]));
   }
 }
 
 unsigned grid_for(int64_t total) {
   const int64_t n = ceil_div(total, kThreads);
   return unsigned(n < 256 * 64 ? n : 256 * 64);
+}
+
+template <int DT, int P, bool BIG>
+hipError_t launch_convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
+  const int64_t total = a.rows * per_row, groups = ceil_div(total, kThreads * P);
+  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  const Pieces<BIG> n{per_row, total, FastDiv::make(BIG ? 1u : uint32_t(per_row))};
+  if (quantize) hipLaunchKernelGGL((mx4_quantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n);
+  else hipLaunchKernelGGL((mx4_dequantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n);
+  return hipGetLastError();
+}
+// Four pieces per lane where that still leaves eight workgroups for every compute unit.
+template <int DT>
+hipError_t convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
+  const int64_t total = a.rows * per_row;
+  if (total == 0) return hipSuccess;
+  if (total > 0x7fffffff) return launch_convert<DT, 4, true>(a, per_row, quantize, s);
+  if (total >= int64_t(256) * 8 * 4 * kThreads) return launch_convert<DT, 4, false>(a, per_row, quantize, s);
+  return launch_convert<DT, 1, false>(a, per_row, quantize, s);
 }
 
 // Lanes run over (batch, token, head, piece of 8 numbers); blockIdx.y: keys or values.
@@ -138,17 +193,33 @@ __device__ __forceinline__ Token place_of(const Mx4TokenArgs& a, int64_t b, int6
   return k;
 }
 
-template <int DT, bool WRITE>
-__global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, int64_t total) {
+struct TokenDivs {
+  FastDiv pieces, heads, tokens;
+};
+template <int DT, bool WRITE, bool BIG>
+__global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, int64_t total, TokenDivs by) {
   const uint32_t pieces = uint32_t(a.cache.dim / 8);
   const bool values = blockIdx.y;
   void* plain = values ? a.v : a.k;
   for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
-    int64_t r = at / pieces;
-    const uint32_t piece = uint32_t(at - r * pieces);
-    const int64_t token = r / a.cache.heads;
-    const int head = int(r - token * a.cache.heads);
-    const int64_t b = token / a.tokens, t = token - b * a.tokens;
+    uint32_t piece;
+    int head;
+    int64_t b, t;
+    if constexpr (BIG) {
+      const int64_t r = at / pieces, token = r / a.cache.heads;
+      piece = uint32_t(at - r * pieces);
+      head = int(r - token * a.cache.heads);
+      b = token / a.tokens;
+      t = token - b * a.tokens;
+    } else {
+      uint32_t r, token, of, seq, in;
+      by.pieces.divmod(uint32_t(at), &r, &piece);
+      by.heads.divmod(r, &token, &of);
+      by.tokens.divmod(token, &seq, &in);
+      head = int(of);
+      b = seq;
+      t = in;
+    }
     const Token place = place_of(a, b, t, head, WRITE);
     const uint32_t codes = values ? a.cache.value(place.slot, piece) : a.cache.key(place.slot) + piece * 4;
     const uint32_t scale = values ? a.cache.value_scale(place.slot, piece / 4) : a.cache.key_scale(place.slot, piece / 4);
@@ -172,32 +243,34 @@ __global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, in
   }
 }
 
-template <bool WRITE>
-hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {
+template <int DT, bool WRITE>
+hipError_t launch_tokens_of(const Mx4TokenArgs& a, hipStream_t s) {
   const int64_t total = a.batch * a.tokens * a.cache.heads * (a.cache.dim / 8);
   if (total == 0) return hipSuccess;
   const dim3 grid(grid_for(total), 2);
-  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_tokens_kernel<GS_BF16, WRITE>), grid, dim3(kThreads), 0, s, a, total);
-  else hipLaunchKernelGGL((mx4_tokens_kernel<GS_F32, WRITE>), grid, dim3(kThreads), 0, s, a, total);
+  if (total > 0x7fffffff) {
+    hipLaunchKernelGGL((mx4_tokens_kernel<DT, WRITE, true>), grid, dim3(kThreads), 0, s, a, total, TokenDivs{});
+  } else {
+    const TokenDivs by{FastDiv::make(uint32_t(a.cache.dim / 8)), FastDiv::make(uint32_t(a.cache.heads)), FastDiv::make(uint32_t(a.tokens))};
+    hipLaunchKernelGGL((mx4_tokens_kernel<DT, WRITE, false>), grid, dim3(kThreads), 0, s, a, total, by);
+  }
   return hipGetLastError();
+}
+template <bool WRITE>
+hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {
+  return a.dtype == GS_BF16 ? launch_tokens_of<GS_BF16, WRITE>(a, s) : launch_tokens_of<GS_F32, WRITE>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_mx4_quantize(const Mx4ConvertArgs& a, hipStream_t s) {
-  const int64_t per_row = mx4_scale_pitch(a.cols) * 4, total = a.rows * per_row;
-  if (total == 0) return hipSuccess;
-  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_quantize_kernel<GS_BF16>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
-  else hipLaunchKernelGGL((mx4_quantize_kernel<GS_F32>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
-  return hipGetLastError();
+  const int64_t per_row = mx4_scale_pitch(a.cols) * 4;
+  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, true, s) : convert<GS_F32>(a, per_row, true, s);
 }
 
 hipError_t launch_mx4_dequantize(const Mx4ConvertArgs& a, hipStream_t s) {
-  const int64_t per_row = ceil_div(a.cols, 8), total = a.rows * per_row;
-  if (total == 0) return hipSuccess;
-  if (a.dtype == GS_BF16) hipLaunchKernelGGL((mx4_dequantize_kernel<GS_BF16>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
-  else hipLaunchKernelGGL((mx4_dequantize_kernel<GS_F32>), dim3(grid_for(total)), dim3(kThreads), 0, s, a, per_row, total);
-  return hipGetLastError();
+  const int64_t per_row = ceil_div(a.cols, 8);
+  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, false, s) : convert<GS_F32>(a, per_row, false, s);
 }
 
 hipError_t launch_mx4_append(const Mx4TokenArgs& a, hipStream_t s) { return launch_tokens<true>(a, s); }
