@@ -415,66 +415,90 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
       }
     } else {
       const int64_t slot = (task * a.parts + part) * kRows + u * 16 + rr;
-      float* dst = a.partial + slot * (D + 2);
-      if (d0 == 0) {
-        dst[0] = top;
-        dst[1] = total;
-      }
+      float* dst = a.partial + slot * (D + kPartHead);
+      if (d0 == 0) *reinterpret_cast<f32x2_t*>(dst) = f32x2_t{top, total};
 #pragma unroll
-      for (int d = 0; d < D / 16; d += 2) *reinterpret_cast<f32x2_t*>(dst + 2 + d0 + d) = f32x2_t{x[d], x[d + 1]};
+      for (int d = 0; d < D / 16; d += 2) *reinterpret_cast<f32x2_t*>(dst + kPartHead + d0 + d) = f32x2_t{x[d], x[d + 1]};
     }
   }
 }
 
-// Joins the parts of a row: one wave per row, a lane for each part's maximum and sum, then two numbers per lane.
-template <int D, int QT>
-__global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, int64_t total_rows) {
-  constexpr int kRows = 16 * QT;
-  const int lane = threadIdx.x & 63;
-  const int64_t at = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= total_rows) return;
+// Joins the parts of rows, D / 4 lanes to a row, four parts' loads under way at a time.  Up to kMaxParts / 8 parts a workgroup has as many rows as
+// it has lanes for; above, one row (SPLIT), whose parts are dealt to these groups of lanes and joined through LDS.
+template <int D, int kRows, bool SPLIT>
+__global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, int32_t total_rows) {
+  constexpr int LPR = D / 4, G = 256 / LPR;
+  __shared__ f32x4 shared_x[SPLIT ? G : 1][LPR];
+  __shared__ float shared_ml[SPLIT ? G : 1][2];
+  const int group = threadIdx.x / LPR, d = threadIdx.x % LPR * 4;
+  const int32_t at = SPLIT ? int32_t(blockIdx.x) : int32_t(blockIdx.x) * G + group;
+  if (at >= total_rows || (!SPLIT && group >= G)) return;
   const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
-  const int64_t bh = at / rows;
-  const int32_t row = int32_t(at - bh * rows), row_tile = row / kRows;
-  const int64_t b = bh / a.cache.heads;
-  const int head = int(bh - b * a.cache.heads);
+  const int32_t bh = at / rows, row = at - bh * rows, row_tile = row / kRows;
+  const int32_t b = bh / a.cache.heads, head = bh - b * a.cache.heads;
   const int32_t row0 = row_tile * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
   const Span span = span_of(a, length_of(a, b), row0, row1);
   if (span.parts == 1) return;
-  const float* src = a.partial + ((bh * row_tiles + row_tile) * a.parts * kRows + (row - row0)) * (D + 2);
-  constexpr int64_t kStride = int64_t(kRows) * (D + 2);
-  float m = -__builtin_inff(), l = 0;
-  if (lane < span.parts) {
-    m = src[lane * kStride];
-    l = src[lane * kStride + 1];
-  }
-  float top = m;
+  constexpr int64_t kStride = int64_t(kRows) * (D + kPartHead);
+  const float* const src = a.partial + (int64_t(bh) * row_tiles + row_tile) * a.parts * kStride + (row - row0) * (D + kPartHead);
+  float top = -__builtin_inff(), total = 0;
+  f32x4 x = {0, 0, 0, 0};
+  constexpr int kStep = SPLIT ? G : 1;
+  if (group < G)
+    for (int p0 = SPLIT ? group : 0; p0 < span.parts; p0 += 4 * kStep) {
+      f32x2_t ml[4];
+      f32x4 v[4];
 #pragma unroll
-  for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-  const float f = exp2_fast(m - (top == -__builtin_inff() ? 0.0f : top));
-  float total = lane < span.parts ? f * l : 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        const int p = p0 + i * kStep;
+        ml[i] = f32x2_t{-__builtin_inff(), 0};
+        v[i] = f32x4{0, 0, 0, 0};
+        if (p < span.parts) {
+          ml[i] = *reinterpret_cast<const f32x2_t*>(src + p * kStride);
+          v[i] = *reinterpret_cast<const f32x4*>(src + p * kStride + kPartHead + d);
+        }
+      }
+      const float now = fmaxf(fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), top);
+      const float ref = now == -__builtin_inff() ? 0.0f : now;
+      const float shrink = exp2_fast(top - ref);
+      top = now;
+      total *= shrink;
+      x *= shrink;
 #pragma unroll
-  for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
-  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
-  const int32_t i = row / a.group, h = row - i * a.group;
-  const int64_t dst = ((b * a.queries + i) * a.cache.heads * a.group + int64_t(head) * a.group + h) * D;
-#pragma unroll
-  for (int d0 = 0; d0 < D; d0 += 128) {
-    const int d = d0 + 2 * lane;
-    float x0 = 0, x1 = 0;
-    for (int p = 0; p < span.parts; ++p) {
-      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), p));
-      if (d < D) {
-        const f32x2_t v = *reinterpret_cast<const f32x2_t*>(src + p * kStride + 2 + d);
-        x0 += w * v[0];
-        x1 += w * v[1];
+      for (int i = 0; i < 4; ++i) {
+        const float f = exp2_fast(ml[i][0] - ref);
+        total += f * ml[i][1];
+        x += f * v[i];
       }
     }
-    if (d < D) {
-      if (a.out_dtype == GS_BF16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + dst + d) = pack_bf16x2(x0 * inv, x1 * inv);
-      else *reinterpret_cast<f32x2_t*>(static_cast<float*>(a.out) + dst + d) = f32x2_t{x0 * inv, x1 * inv};
+  if constexpr (SPLIT) {
+    if (group < G) {
+      shared_x[group][d / 4] = x;
+      if (d == 0) {
+        shared_ml[group][0] = top;
+        shared_ml[group][1] = total;
+      }
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 1; i < G; ++i) top = fmaxf(top, shared_ml[i][0]);
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    total = 0;
+    x = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const float f = exp2_fast(shared_ml[i][0] - ref);
+      total += f * shared_ml[i][1];
+      x += f * shared_x[i][d / 4];
     }
   }
+  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+  const int32_t i = row / a.group, h = row - i * a.group;
+  const int64_t dst = ((int64_t(b) * a.queries + i) * a.cache.heads * a.group + int64_t(head) * a.group + h) * D + d;
+  if (a.out_dtype == GS_BF16)
+    *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + dst) = i32x2{int32_t(pack_bf16x2(x[0] * inv, x[1] * inv)), int32_t(pack_bf16x2(x[2] * inv, x[3] * inv))};
+  else *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + dst) = x * inv;
 }
 
 // Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
@@ -503,7 +527,7 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   const int64_t rows = int64_t(a.queries) * a.group;
   const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, kRows) * a.parts;
   const int64_t total_rows = a.batch * a.cache.heads * rows;
-  if (groups > 0x7fffffff || total_rows > 0x7fffffff) return hipErrorInvalidValue;
+  if (groups > 0x7fffffff || total_rows > 0x7fffff00) return hipErrorInvalidValue;
   void (*kernel)(Mx4AttendArgs);
   size_t lds;
   if constexpr (kMany) {
@@ -518,7 +542,9 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kWaves * 64), lds, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
-    hipLaunchKernelGGL((mx4_attend_join_kernel<D, QT>), dim3(unsigned(ceil_div(total_rows, 4))), dim3(256), 0, s, a, total_rows);
+    constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
+    if (a.parts > kMaxParts / 8) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
+    else hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, false>), dim3(unsigned(ceil_div(total_rows, kJoined))), dim3(256), 0, s, a, int32_t(total_rows));
     e = hipGetLastError();
   }
   return e;
@@ -535,7 +561,7 @@ size_t mx4_attend_workspace(const Mx4AttendArgs& given) {
   plan(&a);
   if (a.parts == 1) return 0;
   const int64_t rows = int64_t(a.queries) * a.group;
-  return size_t(a.batch * a.cache.heads * ceil_div(rows, 16 * a.tiles) * a.parts * 16 * a.tiles) * size_t(a.cache.dim + 2) * 4;
+  return size_t(a.batch * a.cache.heads * ceil_div(rows, 16 * a.tiles) * a.parts * 16 * a.tiles) * size_t(a.cache.dim + kPartHead) * 4;
 }
 
 hipError_t launch_mx4_attend(const Mx4AttendArgs& given, hipStream_t s) {

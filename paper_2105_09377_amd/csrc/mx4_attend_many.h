@@ -55,16 +55,21 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
   const int32_t row = first_row + r, qi = row / a.group, qh = row - qi * a.group;
   const int32_t pos = row < rows ? len - a.queries + qi : -1;
   const int64_t row_at = ((int64_t(b) * a.queries + qi) * a.cache.heads + head) * a.group * D + int64_t(qh) * D;
-  // a negative scale turns the signs of the queries, so that the largest score is the largest product
+  // A negative scale turns the signs of the queries and one of zero makes them zero (infinite ones NaN), so that a score is its product
+  // times a positive number: the largest is the largest, and that of a token that is not seen may be set to -infinity before.
   const uint32_t turn = a.scale < 0 ? 0x80008000u : 0u;
-  const float to_log2 = fabsf(a.scale) * 1.44269504088896340736f;
+  const float to_log2 = a.scale == 0 ? 1.0f : fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.17549435e-38f);
   i32x4 q[2 * NB];
 #pragma unroll
   for (int s = 0; s < 2 * NB; ++s) {
     q[s] = i32x4{0, 0, 0, 0};
     if (row < rows) q[s] = *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(a.q) + row_at + s * 16 + h * 8);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[s][i] ^= int32_t(turn);
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x = uint32_t(q[s][i]);
+      if (a.scale == 0) x = pack_bf16x2(__uint_as_float(x << 16) * 0.0f, __uint_as_float(x & 0xffff0000u) * 0.0f);
+      q[s][i] = int32_t(x ^ turn);
+    }
   }
 
   f32x16 o[NB];
@@ -138,7 +143,10 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
         if (__any(wild)) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (((raw_scale[u] >> (8 * j)) & 255u) >= 253u) raw[u][j] = 0;
+            if (((raw_scale[u] >> (8 * j)) & 255u) >= 253u) {
+              raw[u][j] = 0;
+              raw_scale[u] &= ~(255u << (8 * j));
+            }
           if (lane == 0) meta[4 + wave + 4 * u - NB] = 1;
         } else if (lane == 0) {
           meta[4 + wave + 4 * u - NB] = 0;
@@ -146,7 +154,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
         uint32_t d[4][4];                                // [token][pair of numbers]
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t byte = (raw_scale[u] >> (8 * j)) & 255u, x = byte < 253 ? byte << 23 : 0u;
+          const uint32_t x = ((raw_scale[u] >> (8 * j)) & 255u) << 23;
           const i32x4 y = mx4_decode8(uint32_t(raw[u][j]), __uint_as_float(x > 0x00400000u ? x : 0x00400000u));
 #pragma unroll
           for (int c = 0; c < 4; ++c) d[j][c] = uint32_t(y[c]);
@@ -164,7 +172,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
       }
     }
   };
-  const int32_t window = a.window > 0 ? int32_t(a.window) : 0x7fffffff, sinks = int32_t(a.sinks);
+  const int32_t window = a.window > 0 ? int32_t(a.window) : 1 << 30, sinks = int32_t(a.sinks);
   auto sees = [&](int32_t position, int32_t token) {
     return token <= position && (position - token < window || token < sinks);
   };
@@ -173,47 +181,66 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
     const i32x4 meta = *reinterpret_cast<const i32x4*>(buf + S::kBuf);
     const uint32_t pages = __builtin_amdgcn_readfirstlane(meta[0]);
     const bool tame = __builtin_amdgcn_readfirstlane(meta[1] | meta[2]) == 0;
+    // scores: both halves of the tile in turn, their keys requested two steps ahead
     f32x16 s[2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[n][v] = 0;
+    i32x4 kf[3][2];
+    const uint8_t* const keys = buf + r * kKeyRow + h * 16;
+    auto read_keys = [&](auto c_) {
+      constexpr int c = decltype(c_)::value;
 #pragma unroll
-      for (int c = 0; c < 2 * NB; ++c) {
-        const i32x4 k = *reinterpret_cast<const i32x4*>(buf + (n * 32 + r) * kKeyRow + c * 32 + h * 16);
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s[n], 0, 0, 0);
-      }
-    }
+      for (int n = 0; n < 2; ++n) kf[c % 3][n] = *reinterpret_cast<const i32x4*>(keys + n * 32 * kKeyRow + c * 32);
+    };
+    read_keys(std::integral_constant<int, 0>{});
+    read_keys(std::integral_constant<int, 1>{});
+    static_for<2 * NB>([&](auto c_) {
+      constexpr int c = decltype(c_)::value;
+      if constexpr (c + 2 < 2 * NB) read_keys(std::integral_constant<int, c + 2>{});
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[c % 3][n]), __builtin_bit_cast(bf16x8, q[c]), s[n], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    i32x4 vf[2][NB];
+    const uint8_t* const values = buf + kTile * kKeyRow + r * kValueRow + h * 16;
+    auto read_values = [&](auto k_) {                    // 16 tokens
+      constexpr int k = decltype(k_)::value;
+#pragma unroll
+      for (int d = 0; d < NB; ++d) vf[k % 2][d] = *reinterpret_cast<const i32x4*>(values + d * 32 * kValueRow + k * 32);
+    };
+    read_values(std::integral_constant<int, 0>{});
     const bool all_seen = pages == 0x01010101u && token0 + kTile - 1 <= pos_first &&
                           (pos_last - token0 < window || token0 + kTile <= sinks);
-    uint32_t seen = ~0u;                                 // bit 16 n + v
     if (!all_seen) {
-      seen = 0;
+      // tokens that the row sees, of the tile's 64 a bit each, then those of the lane's half: bit 8 (v / 4) + v % 4 of seen
+      auto below = [&](int32_t n) {                      // the first n of 64
+        return n <= 0 ? 0ull : n >= 64 ? ~0ull : ~0ull >> (64 - n);
+      };
+      uint64_t paged = 0;
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int i = 0; i < 4; ++i) paged |= ((pages >> (8 * i)) & 1u) ? 0xffffull << (16 * i) : 0ull;
+      const uint64_t mask = paged & below(pos - token0 + 1) & (~below(pos - token0 - window + 1) | below(sinks - token0));
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int of = 32 * n + 8 * (v / 4) + v % 4;
-          const bool ok = ((pages >> (of / 16 * 8)) & 1u) && sees(pos, token0 + of + 4 * h);
-          seen |= uint32_t(ok) << (16 * n + v);
-        }
+      for (int n = 0; n < 2; ++n) {
+        const uint32_t seen = uint32_t(mask >> (32 * n)) >> (4 * h);
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!(seen & (1u << (8 * (v / 4) + v % 4)))) s[n][v] = -__builtin_inff();
+      }
     }
     float top = -__builtin_inff();
-    if (all_seen) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
-    } else {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) top = fmaxf(top, (seen >> (16 * n + v)) & 1u ? s[n][v] : -__builtin_inff());
-    }
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
     const uint32_t bits = __float_as_uint(top);
     const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
     top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    top = top == -__builtin_inff() ? m : fmaxf(top * to_log2 + kHeadroom, m);      // (a scale of 0 times -infinity is no maximum)
+    top = fmaxf(top * to_log2 + kHeadroom, m);
     const float ref = top == -__builtin_inff() ? 0.0f : top;
     if (__any(top > m)) {
       const float shrink = exp2_fast(m - ref);
@@ -224,30 +251,34 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[d][v] *= shrink;
     }
+    // weights, four at a time; those of the second half between the products of the first
     i32x4 w[2][2];
+    float sum[4] = {0, 0, 0, 0};
+    auto weigh = [&](auto n_, auto i_) {
+      constexpr int n = decltype(n_)::value, i = decltype(i_)::value;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+      for (int v = 4 * i; v < 4 * i + 4; ++v) {
+        s[n][v] = exp2_fast(fmaf(s[n][v], to_log2, -ref));
+        sum[v % 4] += s[n][v];
+      }
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[n][v] = exp2_fast(fmaf(s[n][v], to_log2, -ref));
-      if (!all_seen)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[n][v] = (seen >> (16 * n + v)) & 1u ? s[n][v] : 0.0f;
-      float sum[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sum[v % 4] += s[n][v];
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) w[n][v / 8][v / 2 % 4] = int32_t(pack_bf16x2(s[n][v], s[n][v + 1]));
-    }
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int d = 0; d < NB; ++d) {
-          const i32x4 x = *reinterpret_cast<const i32x4*>(buf + kTile * kKeyRow + (d * 32 + r) * kValueRow + (2 * n + c) * 32 + h * 16);
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w[n][c]), o[d], 0, 0, 0);
-        }
+      for (int v = 4 * i; v < 4 * i + 4; v += 2) w[n][i / 2][v / 2 % 4] = int32_t(pack_bf16x2(s[n][v], s[n][v + 1]));
+    };
+    static_for<4>([&](auto i_) { weigh(std::integral_constant<int, 0>{}, i_); });
+    static_for<4>([&](auto k_) {
+      constexpr int k = decltype(k_)::value;
+      if constexpr (k < 3) read_values(std::integral_constant<int, k + 1>{});
+      static_for<NB>([&](auto d_) {
+        constexpr int d = decltype(d_)::value, slot = k * NB + d;
+        __builtin_amdgcn_sched_barrier(0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % 2][d]), __builtin_bit_cast(bf16x8, w[k / 2][k % 2]), o[d], 0, 0, 0);
+        static_for<4>([&](auto i_) {
+          if constexpr (decltype(i_)::value * NB / 2 == slot) weigh(std::integral_constant<int, 1>{}, i_);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     if (!tame) {
 #pragma unroll 1
       for (int32_t token = token0; token < token0 + kTile && token < span.hi; ++token) {
@@ -328,15 +359,13 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
       }
   } else {
     const int64_t task = int64_t(bh) * row_tiles + row_tile;
-    float* const dst = a.partial + ((task * a.parts + part) * kRows + wave * 32 + r) * (D + 2);
+    float* const dst = a.partial + ((task * a.parts + part) * kRows + wave * 32 + r) * (D + kPartHead);
     if (h == 0) *reinterpret_cast<f32x2_t*>(dst) = f32x2_t{m, total};
 #pragma unroll
     for (int d = 0; d < NB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int j = 0; j < 4; j += 2)
-          *reinterpret_cast<f32x2_t*>(dst + 2 + d * 32 + g * 8 + h * 4 + j) = f32x2_t{o[d][4 * g + j], o[d][4 * g + j + 1]};
+        *reinterpret_cast<f32x4*>(dst + kPartHead + d * 32 + g * 8 + h * 4) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
   }
 }
 

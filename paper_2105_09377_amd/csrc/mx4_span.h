@@ -8,7 +8,8 @@ namespace gs {
 namespace {
 
 constexpr int kTile = 64;            // tokens of a wave's step
-constexpr int kMaxParts = 64;        // the joining kernel has a lane for each
+constexpr int kMaxParts = 64;
+constexpr int kPartHead = 4;         // floats in front of a part's results: its maximum and sum
 // Weights are 2^(score - maximum - kHeadroom): their sum over 2^24 tokens, times the largest number of the format, does not
 // overflow before it is divided by their sum.
 constexpr float kHeadroom = 24.0f;
