@@ -504,8 +504,8 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
 // Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
 void plan(Mx4AttendArgs* a) {
   const int64_t rows = int64_t(a->queries) * a->group;
-  a->tiles = rows > 32 ? 8 : rows > 16 ? 2 : 1;
-  a->least = a->tiles == 8 ? 4 : 8;
+  a->tiles = rows > 128 && a->cache.dim <= 128 ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
+  a->least = a->tiles >= 8 ? 4 : 8;
   const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles);
   int64_t most = a->width * a->cache.page;
   if (a->window > 0) {
@@ -513,7 +513,8 @@ void plan(Mx4AttendArgs* a) {
     most = seen < most ? seen : most;
   }
   const int64_t some = tasks > 0 ? tasks : 1;
-  int64_t parts = a->tiles == 8 ? (512 + some / 2) / some : ceil_div(1024, some);
+  const int64_t groups = a->tiles == 16 || (a->tiles == 8 && a->cache.dim > 128) ? 256 : 512;        // that the chip has at a time
+  int64_t parts = a->tiles >= 8 ? (groups + some / 2) / some : ceil_div(1024, some);
   const int64_t useful = ceil_div(ceil_div(most, kTile), a->least);
   parts = parts < useful ? parts : useful;
   parts = parts < kMaxParts ? parts : kMaxParts;
@@ -522,7 +523,7 @@ void plan(Mx4AttendArgs* a) {
 
 template <int D, int QT>
 hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
-  constexpr bool kMany = QT == 8;
+  constexpr bool kMany = QT >= 8;
   constexpr int kRows = 16 * QT;
   const int64_t rows = int64_t(a.queries) * a.group;
   const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, kRows) * a.parts;
@@ -531,15 +532,15 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   void (*kernel)(Mx4AttendArgs);
   size_t lds;
   if constexpr (kMany) {
-    kernel = mx4_attend_many_kernel<D>;
-    lds = ManyShape<D>::kLds;
+    kernel = mx4_attend_many_kernel<D, QT / 2>;
+    lds = ManyShape<D, QT / 2>::kLds;
   } else {
     kernel = mx4_attend_kernel<D, QT>;
     lds = AttendShape<D, QT>::kLds;
   }
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kWaves * 64), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kMany ? QT * 32 : kWaves * 64), lds, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
@@ -551,6 +552,8 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
 }
 template <int D>
 hipError_t launch_d(const Mx4AttendArgs& a, hipStream_t s) {
+  if constexpr (D <= 128)
+    if (a.tiles == 16) return launch<D, 16>(a, s);
   return a.tiles == 1 ? launch<D, 1>(a, s) : a.tiles == 2 ? launch<D, 2>(a, s) : launch<D, 8>(a, s);
 }
 

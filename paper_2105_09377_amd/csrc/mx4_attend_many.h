@@ -1,6 +1,6 @@
 // Attention over the 4-bit cache for many rows: prompts, and chunks of them over what was cached before.
 //
-// A workgroup has 128 rows, 32 per wave, that share a cache head, and walks the tokens in tiles of 64 that all of its waves use: the
+// A workgroup has 128 or 256 rows, 32 per wave, that share a cache head, and walks the tokens in tiles of 64 that all of its waves use: the
 // tile's codes are converted to bfloat16 once (exactly) into LDS, the next tile's while this one is multiplied, the one
 // behind that on its way into registers.  With r = lane % 32, h = lane / 32 (32x32x16 bfloat16):
 //   scores: 32 tokens x 32 rows per product.  Keys lie in LDS as they are, token after token.  Lane (r, h) receives the scores of
@@ -16,20 +16,21 @@ namespace gs {
 
 namespace {
 
-template <int D>
+template <int D, int NW>
 struct ManyShape {
   static constexpr int NB = D / 32;                      // blocks of a token; 64 units of 16 bytes of a tile's keys each, and of its values
-  static constexpr int U = (2 * NB + 3) / 4;             // units of a lane
+  static constexpr int U = (2 * NB + NW - 1) / NW;       // units of a lane
   static constexpr int kKeyRow = 2 * D + 16, kValueRow = 2 * kTile + 16;
   static constexpr int kBuf = kTile * kKeyRow + D * kValueRow;
   static constexpr int kMeta = 16;                       // bytes: 0-3 whether a run of 16 tokens has a page, 4-11 scales of 2^126 and more
-  static constexpr int kRows = 128;
-  static constexpr size_t kLds = 2 * (kBuf + kMeta);
+  static constexpr int kRows = 32 * NW;
+  static constexpr int kBufs = NW == 8 || D == 64 ? 3 : 2;
+  static constexpr size_t kLds = kBufs * (kBuf + kMeta);
 };
 
-template <int D>
-__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(Mx4AttendArgs a) {
-  using S = ManyShape<D>;
+template <int D, int NW>
+__global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_attend_many_kernel(Mx4AttendArgs a) {
+  using S = ManyShape<D, NW>;
   constexpr int NB = S::NB, U = S::U, kRows = S::kRows, kKeyRow = S::kKeyRow, kValueRow = S::kValueRow;
   extern __shared__ __attribute__((aligned(16))) uint8_t lds_many[];
 
@@ -86,16 +87,16 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
   uint32_t have = 0;                                     // units of `raw` whose token has a page
   i32x4 raw[U];
   uint32_t raw_scale[U];
-  auto key_unit = [&](int u) { return wave + 4 * u < NB; };
-  auto value_unit = [&](int u) { return wave + 4 * u >= NB && wave + 4 * u < 2 * NB; };
-  auto lane_of = [&](int u) { return (wave + 4 * u < NB ? wave + 4 * u : wave + 4 * u - NB) * 64 + lane; };
+  auto key_unit = [&](int u) { return wave + NW * u < NB; };
+  auto value_unit = [&](int u) { return wave + NW * u >= NB && wave + NW * u < 2 * NB; };
+  auto lane_of = [&](int u) { return (wave + NW * u < NB ? wave + NW * u : wave + NW * u - NB) * 64 + lane; };
   auto token_of = [&](int u) { return key_unit(u) ? lane_of(u) / NB : lane_of(u) % 16 * 4; };
   auto find = [&](int32_t i) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       ids[u] = -1;
       const int32_t token = span.token(i) + token_of(u);
-      if (i < stop && wave + 4 * u < 2 * NB && token < span.hi) {
+      if (i < stop && wave + NW * u < 2 * NB && token < span.hi) {
         uint32_t entry, slot;
         a.cache.by_page.divmod(uint32_t(token), &entry, &slot);
         ids[u] = table[entry];
@@ -147,9 +148,9 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
               raw[u][j] = 0;
               raw_scale[u] &= ~(255u << (8 * j));
             }
-          if (lane == 0) meta[4 + wave + 4 * u - NB] = 1;
+          if (lane == 0) meta[4 + wave + NW * u - NB] = 1;
         } else if (lane == 0) {
-          meta[4 + wave + 4 * u - NB] = 0;
+          meta[4 + wave + NW * u - NB] = 0;
         }
         uint32_t d[4][4];                                // [token][pair of numbers]
 #pragma unroll
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
     }
   };
 
-  if (threadIdx.x < 2) *reinterpret_cast<i32x4*>(lds_many + threadIdx.x * (S::kBuf + S::kMeta) + S::kBuf) = i32x4{0, 0, 0, 0};
+  if (threadIdx.x < S::kBufs) *reinterpret_cast<i32x4*>(lds_many + threadIdx.x * (S::kBuf + S::kMeta) + S::kBuf) = i32x4{0, 0, 0, 0};
   __syncthreads();
   if (begin < stop) {
     find(begin);
@@ -324,20 +325,23 @@ __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) mx4_attend_many_kernel(
     find(begin + 1);
     load(begin + 1);
     find(begin + 2);
-    __syncthreads();
-    int buf = 0;
+    // With three buffers the barrier stands between the conversion of the next tile and the products of this one: a wave may be
+    // ahead of another by almost a tile.  With two it stands behind the products, whose buffer the next conversion fills.
+    if (S::kBufs == 2) __syncthreads();
+    uint32_t buf = 0;
     for (int32_t i = begin; i < stop; ++i) {
+      const uint32_t next = buf + (S::kBuf + S::kMeta) == S::kLds ? 0 : buf + (S::kBuf + S::kMeta);
       if (i + 1 < stop) {
-        convert(lds_many + (buf ^ 1) * (S::kBuf + S::kMeta));
+        convert(lds_many + next);
         load(i + 2);
         find(i + 3);
       }
+      if (S::kBufs == 3) __syncthreads();
       const int32_t token0 = span.token(i);
-      const bool any_seen = active && token0 <= pos_last &&
-                            (pos_first - (token0 + kTile - 1) < window || token0 < sinks);
-      if (any_seen) compute(lds_many + buf * (S::kBuf + S::kMeta), token0);
-      __syncthreads();
-      buf ^= 1;
+      const bool any_seen = active && token0 <= pos_last && (pos_first - (token0 + kTile - 1) < window || token0 < sinks);
+      if (any_seen) compute(lds_many + buf, token0);
+      if (S::kBufs == 2) __syncthreads();
+      buf = next;
     }
   }
 
