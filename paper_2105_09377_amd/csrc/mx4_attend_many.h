@@ -74,7 +74,12 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
   }
 
   f32x16 o[NB];
-  float m = -__builtin_inff(), l = 0;
+  // The weights' sum: a product of 4x4x4 with ones gives a lane the sum of the four numbers that it brings (each of the four results).
+  // The rounded weights are summed, those that the values are multiplied with.
+  typedef short bf16x4_bits __attribute__((ext_vector_type(4)));
+  constexpr i32x2 kOnes = {0x3f803f80, 0x3f803f80};
+  float m = -__builtin_inff();
+  f32x4 l = {0, 0, 0, 0};
 #pragma unroll
   for (int d = 0; d < NB; ++d)
 #pragma unroll
@@ -254,16 +259,16 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
     }
     // weights, four at a time; those of the second half between the products of the first
     i32x4 w[2][2];
-    float sum[4] = {0, 0, 0, 0};
     auto weigh = [&](auto n_, auto i_) {
       constexpr int n = decltype(n_)::value, i = decltype(i_)::value;
 #pragma unroll
       for (int v = 4 * i; v < 4 * i + 4; ++v) {
         s[n][v] = exp2_fast(fmaf(s[n][v], to_log2, -ref));
-        sum[v % 4] += s[n][v];
       }
 #pragma unroll
       for (int v = 4 * i; v < 4 * i + 4; v += 2) w[n][i / 2][v / 2 % 4] = int32_t(pack_bf16x2(s[n][v], s[n][v + 1]));
+      const i32x2 four = {w[n][i / 2][2 * i % 4], w[n][i / 2][2 * i % 4 + 1]};
+      l = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(bf16x4_bits, kOnes), __builtin_bit_cast(bf16x4_bits, four), l, 0, 0, 0);
     };
     static_for<4>([&](auto i_) { weigh(std::integral_constant<int, 0>{}, i_); });
     static_for<4>([&](auto k_) {
@@ -279,7 +284,6 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
         __builtin_amdgcn_sched_barrier(0);
       });
     });
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     if (!tame) {
 #pragma unroll 1
       for (int32_t token = token0; token < token0 + kTile && token < span.hi; ++token) {
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
     }
   }
 
-  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[0]), __float_as_uint(l[0]), false, false);
   const float total = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
   if (row >= rows) return;
   if (span.parts == 1) {
