@@ -165,7 +165,7 @@ int attend_args(const gs_ap* q, const gs_mx4_cache* c, const gs_ap* table, int64
   a->table = static_cast<const int32_t*>(table->data);
   a->q = q->data;
   a->batch = q->shape[0];
-  a->width = table->shape[1];
+  a->width = c->n_pages > 0 ? table->shape[1] : 0;     // (without pages no sequence has a token, and nothing of the cache is read)
   a->queries = int32_t(q->shape[1]);
   a->group = int32_t(group);
   const int64_t most = a->width * c->page_size;     // a window of everything is none

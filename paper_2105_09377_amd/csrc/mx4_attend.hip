@@ -44,7 +44,7 @@ __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&out)[N]
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      const i32x4 v = reinterpret_cast<const i32x4*>(p)[i];
+      const i32x4 v = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p) + i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) out[4 * i + j] = uint32_t(v[j]);
     }
@@ -72,24 +72,39 @@ struct AttendShape {
 };
 
 template <int D, int QT>
-__global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kernel(Mx4AttendArgs a) {
+__global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1) mx4_attend_kernel(Mx4AttendArgs a) {
   using S = AttendShape<D, QT>;
   constexpr int C = S::C, KS = S::KS, VP = S::VP, kRows = S::kRows, kRow = S::kRow;
   extern __shared__ __attribute__((aligned(16))) float lds[];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  // workgroup -> (sequence and cache head, row tile, part)
-  const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
-  uint32_t at = blockIdx.x;
-  const uint32_t part = at % uint32_t(a.parts);
-  at /= uint32_t(a.parts);
-  const uint32_t row_tile = at % uint32_t(row_tiles), bh = at / uint32_t(row_tiles);
-  const uint32_t b = bh / uint32_t(a.cache.heads), head = bh - b * uint32_t(a.cache.heads);
-  const int32_t row0 = int32_t(row_tile) * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
+  // workgroup -> sequence, cache head and part; there is one row tile
+  const int32_t rows = a.queries * a.group, row0 = 0, row1 = rows - 1;
+  uint32_t b, head, part;
+  Cut cut;
+  if (a.slots) {
+    const Shares all = shares_of(a, lane);
+    const int32_t slot = int32_t(blockIdx.x / uint32_t(a.cache.heads));
+    head = blockIdx.x - uint32_t(slot) * uint32_t(a.cache.heads);
+    const uint64_t mine = __ballot(slot >= all.before && slot < all.before + all.parts);
+    if (mine == 0) return;
+    b = uint32_t(__builtin_ctzll(mine));
+    cut.per = all.per;
+    cut.parts = __builtin_amdgcn_readlane(all.parts, int(b));
+    part = uint32_t(slot - __builtin_amdgcn_readlane(all.before, int(b)));
+  } else {
+    const uint32_t task = blockIdx.x / uint32_t(a.parts);
+    part = blockIdx.x - task * uint32_t(a.parts);
+    b = task / uint32_t(a.cache.heads);
+    head = task - b * uint32_t(a.cache.heads);
+  }
   const int32_t len = length_of(a, b);
   const Span span = span_of(a, len, row0, row1);
-  if (int32_t(part) >= span.parts) return;
-  const int32_t begin = int32_t(part) * span.per, stop = begin + span.per < span.total ? begin + span.per : span.total;
+  if (!a.slots) {
+    cut = cut_alike(a, span.total, 0);
+    if (int32_t(part) >= cut.parts) return;
+  }
+  const int32_t begin = int32_t(part) * cut.per, stop = begin + cut.per < span.total ? begin + cut.per : span.total;
 
   // the rows' queries, as the scores' products want them, and positions
   i32x4 q[QT][C];
@@ -103,44 +118,52 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
     pos[t] = ok ? len - a.queries + i : -1;
     const uint16_t* src = static_cast<const uint16_t*>(a.q) + (int64_t(b) * a.queries + i) * q_row + (int64_t(head) * a.group + h) * D + g * (D / 4);
 #pragma unroll
-    for (int c = 0; c < C; ++c) q[t][c] = ok ? *reinterpret_cast<const i32x4*>(src + 8 * c) : i32x4{0, 0, 0, 0};
+    for (int c = 0; c < C; ++c) q[t][c] = ok ? scaled_signs(*reinterpret_cast<const i32x4*>(src + 8 * c), a.scale) : i32x4{0, 0, 0, 0};
   }
   const int32_t pos_first = len - a.queries + row0 / a.group, pos_last = len - a.queries + row1 / a.group;
-  const float to_log2 = a.scale * 1.44269504088896340736f;
+  const float to_log2 = positive_scale(a.scale);
 
-  f32x4 o[QT][VP][8];
-  float m[QT], l[QT];
+  f32x4 o[QT][VP][8], l[QT];
+  float m[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     m[t] = -__builtin_inff();
-    l[t] = 0;
+    l[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int p = 0; p < VP; ++p)
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[t][p][j] = f32x4{0, 0, 0, 0};
   }
 
-  // Where the 4 runs of 16 tokens of a tile lie (wave-uniform).
+  // Where the 4 runs of 16 tokens of a tile lie (wave-uniform).  Without branches: a run that has no page, or lies behind the last token that
+  // a row sees, is read from another place of the cache, and its scores are set to -infinity.
   struct Place {
-    const uint8_t* block[4];         // null: no page
+    const uint8_t* block[4];
     uint32_t slot[4];
+    uint32_t pages;                  // bit n: run n has a page
     int32_t token;
   };
   const int32_t* table = a.table + int64_t(b) * a.width;
-  auto find = [&](int32_t i) {
+  const int32_t last_run = (span.hi - 1) & ~15;
+  auto run_of = [&](int32_t i, int n) {
+    const int32_t token = span.token(i < stop ? i : stop - 1) + 16 * n;
+    return token < last_run ? token : last_run;
+  };
+  auto find = [&](int32_t i, int32_t (&ids)[4]) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) ids[n] = table[a.cache.by_page.div(uint32_t(run_of(i, n)))];
+  };
+  auto place = [&](int32_t i, const int32_t (&ids)[4]) {
     Place w;
     w.token = span.token(i);
+    w.pages = 0;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const int32_t token = w.token + 16 * n;
-      w.block[n] = nullptr;
-      w.slot[n] = 0;
-      if (token < span.hi) {
-        uint32_t entry;
-        a.cache.by_page.divmod(uint32_t(token), &entry, &w.slot[n]);
-        const int32_t id = table[entry];
-        if (id >= 0 && id < a.cache.n_pages) w.block[n] = a.cache.block(id, int(head));
-      }
+      const uint32_t run = uint32_t(run_of(i, n));
+      w.slot[n] = run - a.cache.by_page.div(run) * uint32_t(a.cache.page);
+      const bool there = ids[n] >= 0 && ids[n] < a.cache.n_pages;
+      w.pages |= uint32_t(there) << n;
+      w.block[n] = a.cache.block(there ? ids[n] : 0, int(head));
     }
     return w;
   };
@@ -155,17 +178,10 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
   auto load_keys = [&](const Place& w, Keys& t) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      if (w.block[n]) {
-        load_dwords<C>(w.block[n] + w.slot[n] * (D / 2) + uint32_t(r * (D / 2) + g * (D / 8)), t.k[n]);
-        const uint8_t* ks = w.block[n] + page * D + w.slot[n] * C + uint32_t(r * C);
-        t.scale[n][0] = ks[(C * g) / 4];
-        if constexpr (KS == 2) t.scale[n][1] = ks[(C * g + C - 1) / 4];
-      } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c) t.k[n][c] = 0;
-#pragma unroll
-        for (int c = 0; c < KS; ++c) t.scale[n][c] = 127;
-      }
+      load_dwords<C>(w.block[n] + w.slot[n] * (D / 2) + uint32_t(r * (D / 2) + g * (D / 8)), t.k[n]);
+      const uint8_t* ks = w.block[n] + page * D + w.slot[n] * C + uint32_t(r * C);
+      t.scale[n][0] = ks[(C * g) / 4];
+      if constexpr (KS == 2) t.scale[n][1] = ks[(C * g + C - 1) / 4];
     }
   };
   auto load_values = [&](const Place& w, Values& t) {
@@ -173,17 +189,14 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int p = 0; p < VP; ++p) {
-        const int piece = 16 * p + r;
-        t.v[n][p] = i32x4{0, 0, 0, 0};
-        t.scale[n][p] = 0x7f7f7f7fu;
-        if (w.block[n] && (D / 8 - 16 * p >= 16 || piece < D / 8)) {
-          t.v[n][p] = *reinterpret_cast<const i32x4*>(w.block[n] + page * (D / 2) + (w.slot[n] / 4 + g) * (D * 2) + piece * 16);
-          t.scale[n][p] = *reinterpret_cast<const uint32_t*>(w.block[n] + page * (D + C) + ((w.slot[n] / 4 + g) * C + piece / 4) * 4);
-        }
+        const int piece = D / 8 - 16 * p >= 16 || 16 * p + r < D / 8 ? 16 * p + r : D / 8 - 1;
+        t.v[n][p] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(w.block[n] + page * (D / 2) + w.slot[n] * (D / 2) + uint32_t(g * (D * 2) + piece * 16)));
+        t.scale[n][p] = *reinterpret_cast<const uint32_t*>(w.block[n] + page * (D + C) + w.slot[n] * C + uint32_t(g * (C * 4) + piece / 4 * 4));
       }
   };
+  const int32_t window = a.window > 0 ? int32_t(a.window) : 1 << 30, sinks = int32_t(a.sinks);
   auto sees = [&](int32_t position, int32_t token) {
-    return token <= position && (a.window == 0 || position - token < a.window || token < a.sinks);
+    return token <= position && (position - token < window || token < sinks);
   };
 
   // A tile: the next one's keys are requested once this one's are used up, and its values likewise, into the same registers.
@@ -209,28 +222,26 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
       __builtin_amdgcn_sched_barrier(0);               // (conversions ahead of their use cost registers)
     }
     if (more) load_keys(next, keys);
-    const bool all_seen = at.block[0] && at.block[1] && at.block[2] && at.block[3] && at.token + kTile - 1 <= pos_first &&
-                          (a.window == 0 || pos_last - at.token < a.window || at.token + kTile <= a.sinks);
+    const bool all_seen = at.pages == 15u && at.token + kTile - 1 <= pos_first && (pos_last - at.token < window || at.token + kTile <= sinks);
     // weights, as the products with the values want them: p[row tile][half of the tile]
     i32x4 w[QT][2];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-      float e[16];
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[4 * n + i] = s[u][n][i] * to_log2;
       if (!all_seen) {
+        uint64_t paged = 0;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) paged |= (at.pages >> n) & 1u ? 0xffffull << (16 * n) : 0ull;
+        const uint64_t mask = (paged & seen_tokens(pos[u], at.token, window, sinks)) >> (4 * g);
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!at.block[n] || !sees(pos[u], at.token + 16 * n + 4 * g + i)) e[4 * n + i] = -__builtin_inff();
+            if (!((mask >> (16 * n + i)) & 1u)) s[u][n][i] = -__builtin_inff();
       }
-      float top = e[0];
+      float top = s[u][0][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, e[i]);
-      top = fmaxf(max_over_g(top) + kHeadroom, m[u]);
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[u][i / 4][i % 4]);
+      top = fmaxf(max_over_g(top) * to_log2 + kHeadroom, m[u]);
       const float ref = top == -__builtin_inff() ? 0.0f : top;
       if (__any(top > m[u])) {
         const float shrink = exp2_fast(m[u] - ref);
@@ -242,15 +253,14 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
           for (int j = 0; j < 8; ++j) o[u][p][j] *= shrink;
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) e[i] = exp2_fast(e[i] - ref);
-      float sum = 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum += e[i];
-      l[u] += sum;
-#pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[u][h][i] = int32_t(pack_bf16x2(e[8 * h + 2 * i], e[8 * h + 2 * i + 1]));
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 x = s[u][2 * h + i / 2];
+          w[u][h][i] = int32_t(pack_bf16x2(exp2_fast(fmaf(x[2 * i % 4], to_log2, -ref)), exp2_fast(fmaf(x[2 * i % 4 + 1], to_log2, -ref))));
+        }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) l[u] = add_weights(w[u][n / 2][2 * n % 4], w[u][n / 2][2 * n % 4 + 1], l[u]);
     }
     // Scale bytes of 253 and more (2^126, 2^127, NaN) could make infinities or NaN of numbers, and those times a weight of
     // zero would spoil rows that do not see the token: their numbers are zero here and added one by one below.
@@ -345,14 +355,18 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
   };
 
   if (begin + wave < stop) {
+    int32_t i = begin + wave, ids[4];
     Keys keys;
     Values values;
-    Place at = find(begin + wave);
+    find(i, ids);
+    Place at = place(i, ids);
     load_keys(at, keys);
     load_values(at, values);
-    for (int32_t i = begin + wave; i < stop; i += kWaves) {
+    find(i + kWaves, ids);
+    for (; i < stop; i += kWaves) {
       const bool more = i + kWaves < stop;
-      const Place next = more ? find(i + kWaves) : at;
+      const Place next = place(i + kWaves, ids);
+      find(i + 2 * kWaves, ids);
       compute(at, next, more, keys, values);
       if (more) load_values(next, values);
       at = next;
@@ -362,10 +376,9 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
   // join the waves, 16 rows at a time
   float* const my_o = lds + wave * 16 * kRow;
   float* const ml = lds + kWaves * 16 * kRow;            // [wave][row][2]
-  const int64_t task = int64_t(bh) * row_tiles + row_tile;
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
-    const float sum = sum_over_g(l[u]);
+    const float sum = sum_over_g(l[u][0]);
     if (u) __syncthreads();
     if (g == 0) {
       ml[(wave * 16 + r) * 2] = m[u];
@@ -402,7 +415,7 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
     }
     const int32_t row = row0 + u * 16 + rr;
     if (row >= rows) continue;
-    if (span.parts == 1) {
+    if (cut.parts == 1) {
       const float inv = total != 0.0f ? 1.0f / total : 0.0f;
       const int32_t i = row / a.group, h = row - i * a.group;
       const int64_t dst = (int64_t(b) * a.queries + i) * q_row + (int64_t(head) * a.group + h) * D + d0;
@@ -414,7 +427,7 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
           *reinterpret_cast<f32x2_t*>(static_cast<float*>(a.out) + dst + d) = f32x2_t{x[d] * inv, x[d + 1] * inv};
       }
     } else {
-      const int64_t slot = (task * a.parts + part) * kRows + u * 16 + rr;
+      const int64_t slot = int64_t(blockIdx.x) * kRows + u * 16 + rr;
       float* dst = a.partial + slot * (D + kPartHead);
       if (d0 == 0) *reinterpret_cast<f32x2_t*>(dst) = f32x2_t{top, total};
 #pragma unroll
@@ -423,7 +436,7 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? 2 : 1) mx4_attend_kerne
   }
 }
 
-// Joins the parts of rows, D / 4 lanes to a row, four parts' loads under way at a time.  Up to kMaxParts / 8 parts a workgroup has as many rows as
+// Joins the parts of rows, D / 4 lanes to a row, four parts' loads under way at a time.  Up to 8 parts a workgroup has as many rows as
 // it has lanes for; above, one row (SPLIT), whose parts are dealt to these groups of lanes and joined through LDS.
 template <int D, int kRows, bool SPLIT>
 __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, int32_t total_rows) {
@@ -432,20 +445,29 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
   __shared__ float shared_ml[SPLIT ? G : 1][2];
   const int group = threadIdx.x / LPR, d = threadIdx.x % LPR * 4;
   const int32_t at = SPLIT ? int32_t(blockIdx.x) : int32_t(blockIdx.x) * G + group;
-  if (at >= total_rows || (!SPLIT && group >= G)) return;
   const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
-  const int32_t bh = at / rows, row = at - bh * rows, row_tile = row / kRows;
+  const bool ok = at < total_rows && (SPLIT || group < G);
+  const int32_t bh = ok ? at / rows : 0, row = ok ? at - bh * rows : 0, row_tile = row / kRows;
   const int32_t b = bh / a.cache.heads, head = bh - b * a.cache.heads;
   const int32_t row0 = row_tile * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
-  const Span span = span_of(a, length_of(a, b), row0, row1);
-  if (span.parts == 1) return;
-  constexpr int64_t kStride = int64_t(kRows) * (D + kPartHead);
-  const float* const src = a.partial + (int64_t(bh) * row_tiles + row_tile) * a.parts * kStride + (row - row0) * (D + kPartHead);
+  Cut cut;
+  if (a.slots) {                     // (all lanes of a wave take part)
+    const Shares all = shares_of(a, int(threadIdx.x & 63));
+    cut.parts = __shfl(all.parts, b);
+    cut.base = int64_t(__shfl(all.before, b)) * a.cache.heads + head;
+    cut.stride = a.cache.heads;
+  } else {
+    cut = cut_alike(a, span_of(a, length_of(a, b), row0, row1).total, int64_t(bh) * row_tiles + row_tile);
+  }
+  if (!ok || cut.parts == 1) return;
+  constexpr int64_t kResult = int64_t(kRows) * (D + kPartHead);
+  const int64_t stride = cut.stride * kResult;
+  const float* const src = a.partial + cut.base * kResult + (row - row0) * (D + kPartHead);
   float top = -__builtin_inff(), total = 0;
   f32x4 x = {0, 0, 0, 0};
   constexpr int kStep = SPLIT ? G : 1;
   if (group < G)
-    for (int p0 = SPLIT ? group : 0; p0 < span.parts; p0 += 4 * kStep) {
+    for (int p0 = SPLIT ? group : 0; p0 < cut.parts; p0 += 4 * kStep) {
       f32x2_t ml[4];
       f32x4 v[4];
 #pragma unroll
@@ -453,9 +475,9 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
         const int p = p0 + i * kStep;
         ml[i] = f32x2_t{-__builtin_inff(), 0};
         v[i] = f32x4{0, 0, 0, 0};
-        if (p < span.parts) {
-          ml[i] = *reinterpret_cast<const f32x2_t*>(src + p * kStride);
-          v[i] = *reinterpret_cast<const f32x4*>(src + p * kStride + kPartHead + d);
+        if (p < cut.parts) {
+          ml[i] = *reinterpret_cast<const f32x2_t*>(src + p * stride);
+          v[i] = *reinterpret_cast<const f32x4*>(src + p * stride + kPartHead + d);
         }
       }
       const float now = fmaxf(fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), top);
@@ -504,21 +526,32 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
 // Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
 void plan(Mx4AttendArgs* a) {
   const int64_t rows = int64_t(a->queries) * a->group;
-  a->tiles = rows > 128 && a->cache.dim <= 128 ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
+  const bool wide = a->cache.dim > 128;
+  a->tiles = rows > 128 && !wide ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
   a->least = a->tiles >= 8 ? 4 : 8;
-  const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles);
+  a->slots = 0;
+  const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles), some = tasks > 0 ? tasks : 1;
+  // workgroups that the chip has at a time
+  const int64_t groups = a->tiles == 16 || (a->tiles == 8 && wide) || a->tiles == 2 ? 256 : a->tiles == 8 || wide ? 512 : 768;
   int64_t most = a->width * a->cache.page;
   if (a->window > 0) {
     const int64_t seen = a->window + a->queries + (a->sinks < most ? a->sinks : most) + 2 * kTile;
     most = seen < most ? seen : most;
   }
-  const int64_t some = tasks > 0 ? tasks : 1;
-  const int64_t groups = a->tiles == 16 || (a->tiles == 8 && a->cache.dim > 128) ? 256 : 512;        // that the chip has at a time
-  int64_t parts = a->tiles >= 8 ? (groups + some / 2) / some : ceil_div(1024, some);
   const int64_t useful = ceil_div(ceil_div(most, kTile), a->least);
+  int64_t parts = a->tiles >= 8 ? (groups + some / 2) / some : ceil_div(groups, some);
   parts = parts < useful ? parts : useful;
   parts = parts < kMaxParts ? parts : kMaxParts;
   a->parts = int32_t(parts > 1 ? parts : 1);
+  // Lengths that differ are no reason to wait for the longest, where the sequences are few enough for a workgroup to look at all.
+  if (a->parts > 1 && a->tiles <= 2 && a->batch <= 64 && groups / a->cache.heads > a->batch) {
+    const int64_t slots = groups / a->cache.heads;
+    a->slots = int32_t(slots < a->batch * useful ? slots : a->batch * useful);
+  }
+}
+int64_t results_of(const Mx4AttendArgs& a) {     // workgroups
+  if (a.slots) return int64_t(a.slots) * a.cache.heads;
+  return a.batch * a.cache.heads * ceil_div(int64_t(a.queries) * a.group, 16 * a.tiles) * a.parts;
 }
 
 template <int D, int QT>
@@ -526,7 +559,7 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   constexpr bool kMany = QT >= 8;
   constexpr int kRows = 16 * QT;
   const int64_t rows = int64_t(a.queries) * a.group;
-  const int64_t groups = a.batch * a.cache.heads * ceil_div(rows, kRows) * a.parts;
+  const int64_t groups = results_of(a);
   const int64_t total_rows = a.batch * a.cache.heads * rows;
   if (groups > 0x7fffffff || total_rows > 0x7fffff00) return hipErrorInvalidValue;
   void (*kernel)(Mx4AttendArgs);
@@ -544,7 +577,7 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
-    if (a.parts > kMaxParts / 8) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
+    if (a.slots ? a.slots / a.batch >= 8 : a.parts > 8) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
     else hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, false>), dim3(unsigned(ceil_div(total_rows, kJoined))), dim3(256), 0, s, a, int32_t(total_rows));
     e = hipGetLastError();
   }
@@ -563,8 +596,7 @@ size_t mx4_attend_workspace(const Mx4AttendArgs& given) {
   Mx4AttendArgs a = given;
   plan(&a);
   if (a.parts == 1) return 0;
-  const int64_t rows = int64_t(a.queries) * a.group;
-  return size_t(a.batch * a.cache.heads * ceil_div(rows, 16 * a.tiles) * a.parts * 16 * a.tiles) * size_t(a.cache.dim + kPartHead) * 4;
+  return size_t(results_of(a) * 16 * a.tiles) * size_t(a.cache.dim + kPartHead) * 4;
 }
 
 hipError_t launch_mx4_attend(const Mx4AttendArgs& given, hipStream_t s) {

@@ -46,8 +46,9 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
   const int32_t row0 = int32_t(row_tile) * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
   const int32_t len = length_of(a, b);
   const Span span = span_of(a, len, row0, row1);
-  if (int32_t(part) >= span.parts) return;
-  const int32_t begin = int32_t(part) * span.per, stop = begin + span.per < span.total ? begin + span.per : span.total;
+  const Cut cut = cut_alike(a, span.total, int64_t(bh) * row_tiles + row_tile);
+  if (int32_t(part) >= cut.parts) return;
+  const int32_t begin = int32_t(part) * cut.per, stop = begin + cut.per < span.total ? begin + cut.per : span.total;
 
   // the wave's rows
   const int32_t first_row = row0 + wave * 32, last_row = first_row + 31 < rows ? first_row + 31 : rows - 1;
@@ -56,28 +57,15 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
   const int32_t row = first_row + r, qi = row / a.group, qh = row - qi * a.group;
   const int32_t pos = row < rows ? len - a.queries + qi : -1;
   const int64_t row_at = ((int64_t(b) * a.queries + qi) * a.cache.heads + head) * a.group * D + int64_t(qh) * D;
-  // A negative scale turns the signs of the queries and one of zero makes them zero (infinite ones NaN), so that a score is its product
-  // times a positive number: the largest is the largest, and that of a token that is not seen may be set to -infinity before.
-  const uint32_t turn = a.scale < 0 ? 0x80008000u : 0u;
-  const float to_log2 = a.scale == 0 ? 1.0f : fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.17549435e-38f);
+  const float to_log2 = positive_scale(a.scale);
   i32x4 q[2 * NB];
 #pragma unroll
   for (int s = 0; s < 2 * NB; ++s) {
     q[s] = i32x4{0, 0, 0, 0};
-    if (row < rows) q[s] = *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(a.q) + row_at + s * 16 + h * 8);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t x = uint32_t(q[s][i]);
-      if (a.scale == 0) x = pack_bf16x2(__uint_as_float(x << 16) * 0.0f, __uint_as_float(x & 0xffff0000u) * 0.0f);
-      q[s][i] = int32_t(x ^ turn);
-    }
+    if (row < rows) q[s] = scaled_signs(*reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(a.q) + row_at + s * 16 + h * 8), a.scale);
   }
 
   f32x16 o[NB];
-  // The weights' sum: a product of 4x4x4 with ones gives a lane the sum of the four numbers that it brings (each of the four results).
-  // The rounded weights are summed, those that the values are multiplied with.
-  typedef short bf16x4_bits __attribute__((ext_vector_type(4)));
-  constexpr i32x2 kOnes = {0x3f803f80, 0x3f803f80};
   float m = -__builtin_inff();
   f32x4 l = {0, 0, 0, 0};
 #pragma unroll
@@ -223,13 +211,10 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
                           (pos_last - token0 < window || token0 + kTile <= sinks);
     if (!all_seen) {
       // tokens that the row sees, of the tile's 64 a bit each, then those of the lane's half: bit 8 (v / 4) + v % 4 of seen
-      auto below = [&](int32_t n) {                      // the first n of 64
-        return n <= 0 ? 0ull : n >= 64 ? ~0ull : ~0ull >> (64 - n);
-      };
       uint64_t paged = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) paged |= ((pages >> (8 * i)) & 1u) ? 0xffffull << (16 * i) : 0ull;
-      const uint64_t mask = paged & below(pos - token0 + 1) & (~below(pos - token0 - window + 1) | below(sinks - token0));
+      const uint64_t mask = paged & seen_tokens(pos, token0, window, sinks);
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const uint32_t seen = uint32_t(mask >> (32 * n)) >> (4 * h);
@@ -267,8 +252,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
       }
 #pragma unroll
       for (int v = 4 * i; v < 4 * i + 4; v += 2) w[n][i / 2][v / 2 % 4] = int32_t(pack_bf16x2(s[n][v], s[n][v + 1]));
-      const i32x2 four = {w[n][i / 2][2 * i % 4], w[n][i / 2][2 * i % 4 + 1]};
-      l = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(bf16x4_bits, kOnes), __builtin_bit_cast(bf16x4_bits, four), l, 0, 0, 0);
+      l = add_weights(w[n][i / 2][2 * i % 4], w[n][i / 2][2 * i % 4 + 1], l);
     };
     static_for<4>([&](auto i_) { weigh(std::integral_constant<int, 0>{}, i_); });
     static_for<4>([&](auto k_) {
@@ -352,7 +336,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
   const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[0]), __float_as_uint(l[0]), false, false);
   const float total = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
   if (row >= rows) return;
-  if (span.parts == 1) {
+  if (cut.parts == 1) {
     const float inv = total != 0.0f ? 1.0f / total : 0.0f;
 #pragma unroll
     for (int d = 0; d < NB; ++d)
@@ -366,8 +350,7 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
           *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + dst) = f32x4{x0, x1, x2, x3};
       }
   } else {
-    const int64_t task = int64_t(bh) * row_tiles + row_tile;
-    float* const dst = a.partial + ((task * a.parts + part) * kRows + wave * 32 + r) * (D + kPartHead);
+    float* const dst = a.partial + ((cut.base + part) * kRows + wave * 32 + r) * (D + kPartHead);
     if (h == 0) *reinterpret_cast<f32x2_t*>(dst) = f32x2_t{m, total};
 #pragma unroll
     for (int d = 0; d < NB; ++d)

@@ -347,6 +347,31 @@ def test_attend_windows(queries, dim, page, window, sinks):
     check_attention(q, cache, table, torch.tensor([300, 200], dtype=torch.int32), dim ** -0.5, window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("batch,queries,group,dim,window", [(9, 1, 4, 64, 0), (23, 1, 1, 128, 0), (64, 2, 2, 64, 300), (66, 1, 2, 96, 0), (3, 1, 3, 192, 700)])
+def test_attend_lengths_far_apart(batch, queries, group, dim, window):
+    """From nothing to all of the longest: parts of one length, and sequences that have none, one and many of them."""
+    longest = 2300 if batch < 30 else 800
+    cache, table = filled_cache(batch, longest, 1, dim, 16, 425 + batch)
+    q = normal((batch, queries, group, dim), 426)
+    g = torch.Generator().manual_seed(batch)
+    lengths = (longest * torch.rand(batch, generator=g) ** 3).to(torch.int32)
+    lengths[0], lengths[batch // 2], lengths[batch - 1] = longest, 0, longest
+    check_attention(q, cache, table, lengths, dim ** -0.5, window=window, sinks=5 if window else 0)
+
+
+def test_attend_without_pages():
+    cache = gs.mx4_cache(1, 2, 16, 64, DEV)._replace(data=torch.zeros((0, 2, 16 * 64 + 64), dtype=torch.uint8, device=DEV))
+    q = normal((3, 2, 4, 64), 427).to(DEV)
+    table, n = torch.zeros((3, 5), dtype=torch.int32, device=DEV), torch.tensor([80, 0, 7], dtype=torch.int32, device=DEV)
+    for queries in (1, 2):
+        out = torch.full((3, queries, 4, 64), 5.0, dtype=BF, device=DEV)
+        gs.mx4_attend(q[:, :queries].contiguous(), cache, table, n, 0.1, out=out)
+        assert not out.any()
+    many = torch.full((3, 50, 4, 64), 5.0, dtype=BF, device=DEV)
+    gs.mx4_attend(many, cache, table, n, 0.1, out=many)
+    assert not many.any()
+
+
 MANY_ROWS = [  # more than 32 rows of a cache head: tiles of 128 rows, the last of them partly empty
     (1, 33, 1, 1, 64, 16, 33), (2, 100, 2, 4, 64, 16, 400), (1, 129, 1, 1, 128, 32, 200), (2, 64, 1, 3, 96, 16, 1000), (1, 50, 2, 2, 192, 48, 700),
     (1, 70, 1, 2, 256, 16, 600), (3, 130, 1, 1, 64, 64, 1500), (1, 40, 1, 1, 128, 16, 3000), (1, 9, 2, 16, 256, 64, 1300), (2, 257, 1, 1, 96, 128, 257)]
