@@ -1,8 +1,8 @@
 // Conversion to and from microscaled 4-bit floats: whole matrices, and tokens of a paged cache.
 //
 // A scale is the power of two of its block's largest magnitude, over 4 (the largest power of two of e2m1),
-// so a block is read once, reduced over its 32 numbers, and written: 8 numbers per lane, four neighbouring lanes per block,
-// the maximum over them by two lane exchanges.  Bound by memory: n numbers of s bytes move n (s + 17/32).
+// so a block is read once, reduced over its 32 numbers, and written: 16 bytes of numbers per lane where they lie in rows, four (bfloat16) or
+// eight (floats) neighbouring lanes per block, the maximum over them by lane exchanges; 8 numbers per lane of a cache's tokens.  Bound by memory: n numbers of s bytes move n (s + 17/32).
 #include "mx4.h"
 
 namespace gs {
@@ -21,11 +21,12 @@ __device__ __forceinline__ float load_plain(const void* p, int64_t i, std::integ
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
 
-// Eight numbers of a row from element `at` on, zero beyond `left` of them.
-template <int DT>
-__device__ __forceinline__ void load8(const void* row, int64_t at, int64_t left, float (&x)[8]) {
-  if (left >= 8) {
+// N numbers (8 or 4) of a row from element `at` on, zero beyond `left` of them.
+template <int DT, int N>
+__device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_t left, float (&x)[N]) {
+  if (left >= N) {
     if constexpr (DT == GS_BF16) {
+      static_assert(N == 8, "16 bytes");
       const i32x4 v = *reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -34,7 +35,7 @@ __device__ __forceinline__ void load8(const void* row, int64_t at, int64_t left,
       }
     } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < N / 4; ++h) {
         const f32x4_any v = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * h + i] = v[i];
@@ -43,12 +44,13 @@ __device__ __forceinline__ void load8(const void* row, int64_t at, int64_t left,
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = i < left ? load_plain(row, at + i, std::integral_constant<int, DT>{}) : 0.0f;
+  for (int i = 0; i < N; ++i) x[i] = i < left ? load_plain(row, at + i, std::integral_constant<int, DT>{}) : 0.0f;
 }
 
-template <int DT>
-__device__ __forceinline__ void store8(void* row, int64_t at, int64_t left, uint32_t w, float scale) {
+template <int DT, int N>
+__device__ __forceinline__ void store_numbers(void* row, int64_t at, int64_t left, uint32_t w, float scale) {
   if constexpr (DT == GS_BF16) {
+    static_assert(N == 8, "16 bytes");
     uint16_t* dst = static_cast<uint16_t*>(row) + at;
     const i32x4 v = mx4_decode8(w, scale);
     if (left >= 8) {
@@ -60,35 +62,46 @@ __device__ __forceinline__ void store8(void* row, int64_t at, int64_t left, uint
     }
   } else {
     float* dst = static_cast<float*>(row) + at;
-    float x[8];
+    float x[N];
     mx4_decode2_f32<0>(w, scale, x);
     mx4_decode2_f32<1>(w, scale, x + 2);
-    mx4_decode2_f32<2>(w, scale, x + 4);
-    mx4_decode2_f32<3>(w, scale, x + 6);
-    if (left >= 8) {
+    if constexpr (N == 8) {
+      mx4_decode2_f32<2>(w, scale, x + 4);
+      mx4_decode2_f32<3>(w, scale, x + 6);
+    }
+    if (left >= N) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4_any*>(dst + 4 * h) = f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+      for (int h = 0; h < N / 4; ++h) *reinterpret_cast<f32x4_any*>(dst + 4 * h) = f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
     } else {
 #pragma unroll
-      for (int i = 0; i < 7; ++i)
+      for (int i = 0; i < N - 1; ++i)
         if (i < left) dst[i] = x[i];
     }
   }
 }
 
-__device__ __forceinline__ uint32_t block_scale_byte(const float (&x)[8]) {
+// The scale byte of the block that 32 / N neighbouring lanes have.
+template <int N>
+__device__ __forceinline__ uint32_t block_scale_byte(const float (&x)[N]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
     top = top > b ? top : b;
   }
-  return mx4_scale_byte(max_of_4_lanes(top));
+  top = max_of_4_lanes(top);
+  if constexpr (N == 4) {
+    const uint32_t o = __builtin_amdgcn_mov_dpp(top, 0x141, 0xF, 0xF, true);       // the eight lanes in reverse
+    top = top > o ? top : o;
+  }
+  return mx4_scale_byte(top);
 }
 
-// Pieces of 8 numbers of all rows, one after the other: a workgroup takes 256 P of them, a lane P that lie 256 apart, whose loads are
-// all under way before the first is used.  Rows and places in them come from a division by multiplication where all pieces count in 32
+// Pieces of 16 bytes of all rows' numbers, one after the other: a workgroup takes 256 P of them, a lane P that lie 256 apart, whose loads are
+// all under way before the first is used.  Rows and places in them come from a division by multiplication where all pieces count in 31
 // bits (BIG: 64-bit divisions).
+template <int DT>
+constexpr int kNumbers = DT == GS_BF16 ? 8 : 4;
 template <bool BIG>
 struct Pieces {
   int64_t per_row, total;
@@ -106,12 +119,13 @@ struct Pieces {
   }
 };
 
-// A row's pieces are counted up to whole runs of scale bytes (a multiple of 32), the padding written as zeros by the same lanes.
+// A row's pieces are counted up to whole runs of scale bytes, the padding written as zeros by the same lanes.
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  constexpr int N = kNumbers<DT>;
   const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
   int64_t row[P], piece[P];
-  float x[P][8];
+  float x[P][N];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int64_t at = base + p * kThreads;
@@ -119,20 +133,28 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a
     n.place(there ? at : 0, &row[p], &piece[p]);
     if (!there) row[p] = -1;
     const void* const src = static_cast<const uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
-    load8<DT>(src, piece[p] * 8, there ? a.cols - piece[p] * 8 : 0, x[p]);
+    load_numbers<DT, N>(src, piece[p] * N, there ? a.cols - piece[p] * N : 0, x[p]);
   }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const uint32_t byte = block_scale_byte(x[p]);
+    const uint32_t byte = block_scale_byte<N>(x[p]);
     if (row[p] < 0) continue;
-    const int64_t block = piece[p] / 4;
-    if (block < blocks) static_cast<uint32_t*>(a.values)[row[p] * blocks * 4 + piece[p]] = mx4_encode8(x[p], byte);
-    if (piece[p] % 4 == 0) static_cast<uint8_t*>(a.scales)[row[p] * pitch + block] = uint8_t(block < blocks ? byte : 0);
+    const int64_t block = piece[p] / (kMx4Block / N);
+    if (block < blocks) {
+      float eight[8] = {};
+#pragma unroll
+      for (int i = 0; i < N; ++i) eight[i] = x[p][i];
+      const int64_t to = row[p] * blocks * (kMx4Block / N) + piece[p];
+      if constexpr (N == 8) static_cast<uint32_t*>(a.values)[to] = mx4_encode8(eight, byte);
+      else static_cast<uint16_t*>(a.values)[to] = uint16_t(mx4_encode8(eight, byte));
+    }
+    if (piece[p] % (kMx4Block / N) == 0) static_cast<uint8_t*>(a.scales)[row[p] * pitch + block] = uint8_t(block < blocks ? byte : 0);
   }
 }
 
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  constexpr int N = kNumbers<DT>;
   const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
   int64_t row[P], piece[P];
   uint32_t w[P], byte[P];
@@ -140,14 +162,16 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs
   for (int p = 0; p < P; ++p) {
     const int64_t at = base + p * kThreads;
     n.place(at < n.total ? at : 0, &row[p], &piece[p]);
-    w[p] = static_cast<const uint32_t*>(a.values)[row[p] * blocks * 4 + piece[p]];
-    byte[p] = static_cast<const uint8_t*>(a.scales)[row[p] * pitch + piece[p] / 4];
+    const int64_t from = row[p] * blocks * (kMx4Block / N) + piece[p];
+    if constexpr (N == 8) w[p] = static_cast<const uint32_t*>(a.values)[from];
+    else w[p] = static_cast<const uint16_t*>(a.values)[from];
+    byte[p] = static_cast<const uint8_t*>(a.scales)[row[p] * pitch + piece[p] / (kMx4Block / N)];
   }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (base + p * kThreads >= n.total) continue;
     void* const dst = static_cast<uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
-    store8<DT>(dst, piece[p] * 8, a.cols - piece[p] * 8, w[p], mx4_scale(byte[p]));
+    store_numbers<DT, N>(dst, piece[p] * N, a.cols - piece[p] * N, w[p], mx4_scale(byte[p]));
   }
 }
 
@@ -225,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, in
     const uint32_t scale = values ? a.cache.value_scale(place.slot, piece / 4) : a.cache.key_scale(place.slot, piece / 4);
     if constexpr (WRITE) {
       float x[8];
-      load8<DT>(plain, at * 8, 8, x);
+      load_numbers<DT, 8>(plain, at * 8, 8, x);
       const uint32_t byte = block_scale_byte(x);
       if (place.block) {
         *reinterpret_cast<uint32_t*>(place.block + codes) = mx4_encode8(x, byte);
@@ -238,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, in
         w = *reinterpret_cast<const uint32_t*>(place.block + codes);
         s = mx4_scale(place.block[scale]);
       }
-      store8<DT>(plain, at * 8, 8, w, s);
+      store_numbers<DT, 8>(plain, at * 8, 8, w, s);
     }
   }
 }
@@ -264,13 +288,12 @@ hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mx4_quantize(const Mx4ConvertArgs& a, hipStream_t s) {
-  const int64_t per_row = mx4_scale_pitch(a.cols) * 4;
-  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, true, s) : convert<GS_F32>(a, per_row, true, s);
+  const int64_t per_row = mx4_scale_pitch(a.cols) * kMx4Block;
+  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row / 8, true, s) : convert<GS_F32>(a, per_row / 4, true, s);
 }
 
 hipError_t launch_mx4_dequantize(const Mx4ConvertArgs& a, hipStream_t s) {
-  const int64_t per_row = ceil_div(a.cols, 8);
-  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, false, s) : convert<GS_F32>(a, per_row, false, s);
+  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, ceil_div(a.cols, 8), false, s) : convert<GS_F32>(a, ceil_div(a.cols, 4), false, s);
 }
 
 hipError_t launch_mx4_append(const Mx4TokenArgs& a, hipStream_t s) { return launch_tokens<true>(a, s); }
