@@ -175,11 +175,6 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs
   }
 }
 
-unsigned grid_for(int64_t total) {
-  const int64_t n = ceil_div(total, kThreads);
-  return unsigned(n < 256 * 64 ? n : 256 * 64);
-}
-
 template <int DT, int P, bool BIG>
 hipError_t launch_convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
   const int64_t total = a.rows * per_row, groups = ceil_div(total, kThreads * P);
@@ -199,86 +194,176 @@ hipError_t convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipS
   return launch_convert<DT, 1, false>(a, per_row, quantize, s);
 }
 
-// Lanes run over (batch, token, head, piece of 8 numbers); blockIdx.y: keys or values.
-struct Token {
-  uint8_t* block;         // null: no place in the cache
-  uint32_t slot;
-};
-__device__ __forceinline__ Token place_of(const Mx4TokenArgs& a, int64_t b, int64_t t, int head, bool counted) {
-  Token k{nullptr, 0};
-  if (counted && a.counts && t >= a.counts[b]) return k;
-  const int64_t pos = int64_t(a.first[b]) + t;
-  if (pos < 0 || pos >= a.width * a.cache.page) return k;
-  uint32_t entry;
-  a.cache.by_page.divmod(uint32_t(pos), &entry, &k.slot);
-  const int32_t id = a.table[b * a.width + entry];
-  if (id < 0 || id >= a.cache.n_pages) return k;
-  k.block = a.cache.block(id, head);
-  return k;
-}
-
+// Tokens of a cache.  A token's place takes two loads, one behind the other (its sequence's first position, an entry of the table), so a lane has
+// several tokens, whose loads are under way together.  Keys: lanes run over (batch, token, head, piece of 8 numbers), P of them each.
+// Values: over (batch, four places, head, piece), whose codes are 16 bytes of the cache and whose scales are 4.
 struct TokenDivs {
-  FastDiv pieces, heads, tokens;
+  FastDiv pieces, heads, steps;      // steps: tokens of a sequence, or fours of places
 };
-template <int DT, bool WRITE, bool BIG>
-__global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, int64_t total, TokenDivs by) {
-  const uint32_t pieces = uint32_t(a.cache.dim / 8);
-  const bool values = blockIdx.y;
-  void* plain = values ? a.v : a.k;
-  for (int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x; at < total; at += int64_t(gridDim.x) * kThreads) {
-    uint32_t piece;
-    int head;
-    int64_t b, t;
-    if constexpr (BIG) {
-      const int64_t r = at / pieces, token = r / a.cache.heads;
-      piece = uint32_t(at - r * pieces);
-      head = int(r - token * a.cache.heads);
-      b = token / a.tokens;
-      t = token - b * a.tokens;
-    } else {
-      uint32_t r, token, of, seq, in;
-      by.pieces.divmod(uint32_t(at), &r, &piece);
-      by.heads.divmod(r, &token, &of);
-      by.tokens.divmod(token, &seq, &in);
-      head = int(of);
-      b = seq;
-      t = in;
-    }
-    const Token place = place_of(a, b, t, head, WRITE);
-    const uint32_t codes = values ? a.cache.value(place.slot, piece) : a.cache.key(place.slot) + piece * 4;
-    const uint32_t scale = values ? a.cache.value_scale(place.slot, piece / 4) : a.cache.key_scale(place.slot, piece / 4);
-    if constexpr (WRITE) {
-      float x[8];
-      load_numbers<DT, 8>(plain, at * 8, 8, x);
-      const uint32_t byte = block_scale_byte(x);
-      if (place.block) {
-        *reinterpret_cast<uint32_t*>(place.block + codes) = mx4_encode8(x, byte);
-        if (piece % 4 == 0) place.block[scale] = uint8_t(byte);
-      }
-    } else {
-      uint32_t w = 0;
-      float s = 1.0f;
-      if (place.block) {
-        w = *reinterpret_cast<const uint32_t*>(place.block + codes);
-        s = mx4_scale(place.block[scale]);
-      }
-      store_numbers<DT, 8>(plain, at * 8, 8, w, s);
-    }
+template <bool BIG>
+__device__ __forceinline__ void split_item(int64_t at, const TokenDivs& by, int64_t pieces, int64_t heads, int64_t steps, uint32_t* piece, int* head, int64_t* b,
+                                           int64_t* step) {
+  if constexpr (BIG) {
+    const int64_t r = at / pieces, s = r / heads;
+    *piece = uint32_t(at - r * pieces);
+    *head = int(r - s * heads);
+    *b = s / steps;
+    *step = s - *b * steps;
+  } else {
+    uint32_t r, s, of, seq, in;
+    by.pieces.divmod(uint32_t(at), &r, piece);
+    by.heads.divmod(r, &s, &of);
+    by.steps.divmod(s, &seq, &in);
+    *head = int(of);
+    *b = seq;
+    *step = in;
   }
 }
 
+template <int DT, bool WRITE, int P, bool BIG>
+__device__ __forceinline__ void key_tokens(const Mx4TokenArgs& a, int64_t total, const TokenDivs& by) {
+  const int64_t base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
+  float x[P][8];
+  uint32_t piece[P];
+  int head[P];
+  int64_t b[P], pos[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const bool there = base + p * kThreads < total;
+    const int64_t at = there ? base + p * kThreads : 0;
+    int64_t t;
+    split_item<BIG>(at, by, a.cache.dim / 8, a.cache.heads, a.tokens, &piece[p], &head[p], &b[p], &t);
+    if constexpr (WRITE) load_numbers<DT, 8>(a.k, at * 8, 8, x[p]);
+    // below 0: no place
+    pos[p] = there && !(WRITE && a.counts && t >= a.counts[b[p]]) ? int64_t(a.first[b[p]]) + t : -1;
+  }
+  int32_t id[P];
+  uint32_t slot[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    id[p] = -1;
+    slot[p] = 0;
+    if (pos[p] >= 0 && pos[p] < a.width * a.cache.page) {
+      uint32_t entry;
+      a.cache.by_page.divmod(uint32_t(pos[p]), &entry, &slot[p]);
+      id[p] = a.table[b[p] * a.width + entry];
+    }
+  }
+  uint32_t w[P], byte[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const bool placed = id[p] >= 0 && id[p] < a.cache.n_pages;
+    uint8_t* const block = a.cache.block(placed ? id[p] : 0, head[p]);
+    const uint32_t codes = a.cache.key(slot[p]) + piece[p] * 4, scale = a.cache.key_scale(slot[p], piece[p] / 4);
+    if constexpr (WRITE) {
+      byte[p] = block_scale_byte<8>(x[p]);
+      if (!placed) continue;
+      *reinterpret_cast<uint32_t*>(block + codes) = mx4_encode8(x[p], byte[p]);
+      if (piece[p] % 4 == 0) block[scale] = uint8_t(byte[p]);
+    } else {
+      w[p] = 0;
+      byte[p] = 127;
+      if (!placed) continue;
+      w[p] = *reinterpret_cast<const uint32_t*>(block + codes);
+      byte[p] = block[scale];
+    }
+  }
+  if constexpr (!WRITE) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      if (base + p * kThreads < total) store_numbers<DT, 8>(a.k, (base + p * kThreads) * 8, 8, w[p], mx4_scale(byte[p]));
+  }
+}
+
+template <int DT, bool WRITE, bool BIG>
+__device__ __forceinline__ void value_tokens(const Mx4TokenArgs& a, int64_t fours, const TokenDivs& by) {
+  const int64_t at = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (at >= a.batch * fours * a.cache.heads * (a.cache.dim / 8)) return;      // (whole blocks)
+  uint32_t piece;
+  int head;
+  int64_t b, four;
+  split_item<BIG>(at, by, a.cache.dim / 8, a.cache.heads, fours, &piece, &head, &b, &four);
+  const int64_t first = a.first[b], pos = first - (first & 3) + four * 4, t0 = pos - first;
+  const int64_t number = ((b * a.tokens + t0) * a.cache.heads + head) * a.cache.dim + piece * 8, step = int64_t(a.cache.heads) * a.cache.dim;
+  float x[4][8];
+  if constexpr (WRITE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool there = t0 + j >= 0 && t0 + j < a.tokens;
+      load_numbers<DT, 8>(a.v, there ? number + j * step : 0, there ? 8 : 0, x[j]);
+    }
+  }
+  int64_t count = a.tokens;
+  if (WRITE && a.counts && a.counts[b] < count) count = a.counts[b];
+  int32_t id = -1;
+  uint32_t slot = 0;
+  if (pos >= 0 && pos < a.width * a.cache.page) {        // (of all four: pages are multiples of 16)
+    uint32_t entry;
+    a.cache.by_page.divmod(uint32_t(pos), &entry, &slot);
+    id = a.table[b * a.width + entry];
+  }
+  const bool placed = id >= 0 && id < a.cache.n_pages;
+  uint8_t* const block = a.cache.block(placed ? id : 0, head);
+  uint8_t *const codes = block + a.cache.value(slot, piece), *const scales = block + a.cache.value_scale(slot, piece / 4);
+  if constexpr (WRITE) {
+    uint32_t w[4], byte[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      byte[j] = block_scale_byte<8>(x[j]);
+      w[j] = mx4_encode8(x[j], byte[j]);
+    }
+    if (!placed) return;
+    if (t0 >= 0 && t0 + 4 <= count) {
+      *reinterpret_cast<i32x4*>(codes) = i32x4{int32_t(w[0]), int32_t(w[1]), int32_t(w[2]), int32_t(w[3])};
+      if (piece % 4 == 0) *reinterpret_cast<uint32_t*>(scales) = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (t0 + j >= 0 && t0 + j < count) {
+          reinterpret_cast<uint32_t*>(codes)[j] = w[j];
+          if (piece % 4 == 0) scales[j] = uint8_t(byte[j]);
+        }
+    }
+  } else {
+    i32x4 w = {0, 0, 0, 0};
+    uint32_t byte = 0x7f7f7f7fu;
+    if (placed) {
+      w = *reinterpret_cast<const i32x4*>(codes);
+      byte = *reinterpret_cast<const uint32_t*>(scales);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (t0 + j >= 0 && t0 + j < a.tokens) store_numbers<DT, 8>(a.v, number + j * step, 8, uint32_t(w[j]), mx4_scale((byte >> (8 * j)) & 255u));
+  }
+}
+
+template <int DT, bool WRITE, int P, bool BIG>
+__global__ void __launch_bounds__(kThreads) mx4_tokens_kernel(Mx4TokenArgs a, int64_t keys, int64_t fours, TokenDivs by_tokens, TokenDivs by_fours) {
+  if (blockIdx.y == 0) key_tokens<DT, WRITE, P, BIG>(a, keys, by_tokens);
+  else value_tokens<DT, WRITE, BIG>(a, fours, by_fours);
+}
+
+template <int DT, bool WRITE, int P, bool BIG>
+hipError_t launch_tokens_as(const Mx4TokenArgs& a, hipStream_t s) {
+  const int64_t pieces = a.cache.dim / 8, keys = a.batch * a.tokens * a.cache.heads * pieces;
+  const int64_t fours = ceil_div(a.tokens + 3, 4);       // of places, wherever the first token lies in one
+  const int64_t key_groups = ceil_div(keys, kThreads * P), value_groups = ceil_div(a.batch * fours * a.cache.heads * pieces, kThreads);
+  const int64_t groups = key_groups > value_groups ? key_groups : value_groups;
+  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  const FastDiv by_pieces = FastDiv::make(uint32_t(pieces)), by_heads = FastDiv::make(uint32_t(a.cache.heads));
+  const TokenDivs by_tokens{by_pieces, by_heads, FastDiv::make(BIG ? 1u : uint32_t(a.tokens))}, by_fours{by_pieces, by_heads, FastDiv::make(BIG ? 1u : uint32_t(fours))};
+  hipLaunchKernelGGL((mx4_tokens_kernel<DT, WRITE, P, BIG>), dim3(unsigned(groups), 2), dim3(kThreads), 0, s, a, keys, fours, by_tokens, by_fours);
+  return hipGetLastError();
+}
+// Four pieces of keys per lane where that still leaves four workgroups for every compute unit (4 x 4001 tokens of 8 x 128 numbers, keys and values with
+// one per lane: 29.7 us, read back 20.8).
 template <int DT, bool WRITE>
 hipError_t launch_tokens_of(const Mx4TokenArgs& a, hipStream_t s) {
-  const int64_t total = a.batch * a.tokens * a.cache.heads * (a.cache.dim / 8);
-  if (total == 0) return hipSuccess;
-  const dim3 grid(grid_for(total), 2);
-  if (total > 0x7fffffff) {
-    hipLaunchKernelGGL((mx4_tokens_kernel<DT, WRITE, true>), grid, dim3(kThreads), 0, s, a, total, TokenDivs{});
-  } else {
-    const TokenDivs by{FastDiv::make(uint32_t(a.cache.dim / 8)), FastDiv::make(uint32_t(a.cache.heads)), FastDiv::make(uint32_t(a.tokens))};
-    hipLaunchKernelGGL((mx4_tokens_kernel<DT, WRITE, false>), grid, dim3(kThreads), 0, s, a, total, by);
-  }
-  return hipGetLastError();
+  const int64_t keys = a.batch * a.tokens * a.cache.heads * (a.cache.dim / 8);
+  if (keys == 0) return hipSuccess;
+  if (keys > 0x3fffffff) return launch_tokens_as<DT, WRITE, 4, true>(a, s);
+  if (keys >= int64_t(256) * 4 * 4 * kThreads) return launch_tokens_as<DT, WRITE, 4, false>(a, s);
+  return launch_tokens_as<DT, WRITE, 1, false>(a, s);
 }
 template <bool WRITE>
 hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {

@@ -109,6 +109,27 @@ def test_conversions_of_other_splits_and_storage():
         assert gs.mx4_dequantize(e).shape == shape
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(2100, 4001, F32), (4300, 4001, BF)])
+def test_conversions_of_large_matrices(rows, cols, dtype):
+    x = normal((rows, cols), 90, dtype, spread=4.0)
+    m = gs.mx4_quantize(x.to(DEV))
+    packed, scales = mx4.quantize(to_oracle(x))
+    assert np.array_equal(bytes_of(m.values), packed) and np.array_equal(bytes_of(m.scales), scales)
+    same_values(gs.mx4_dequantize(m, out_dtype=dtype), mx4.dequantize(packed, scales, cols))
+
+
+def test_conversions_beyond_32_bits():
+    """More than 2^31 pieces of numbers: the same as row by row."""
+    rows, cols = 70000, 131075
+    x = torch.empty((rows, cols), device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(91))
+    m = gs.mx4_quantize(x)
+    some = [0, 1, 32768, 65535, 65536, 69998, 69999]
+    part = gs.mx4_quantize(x[some].contiguous())
+    assert torch.equal(m.values[some], part.values) and torch.equal(m.scales[some], part.scales)
+    gs.mx4_dequantize(m, out=x)
+    assert torch.equal(x[some], gs.mx4_dequantize(part, out_dtype=F32))
+
+
 # ------------------------------------------------------------------------------------------------
 # contractions
 # ------------------------------------------------------------------------------------------------
@@ -268,6 +289,25 @@ def test_append_and_read(batch, new, heads, dim, page, width, dtype):
         gk, gv = gs.mx4_cache_read(cache, table.to(DEV), first.to(DEV), new, out_dtype=odt)
         for got, x in ((gk, k), (gv, v)):
             same_values(got, mx4.dequantize(*mx4.quantize(to_oracle(x).reshape(-1, dim)), dim).reshape(x.shape))
+
+
+@pytest.mark.parametrize("new,dtype", [(9000, BF), (1 << 22, BF)])
+def test_append_and_read_of_many(new, dtype):
+    """More pieces than one per lane, and than 2^30: read back a few tokens at a time."""
+    heads, dim, page = 8, 256, 4096 if new > 10000 else 64
+    width = (new + 5) // page + 1
+    cache = gs.mx4_cache(width, heads, page, dim, DEV)
+    table = torch.randperm(width, generator=torch.Generator().manual_seed(92)).to(torch.int32).view(1, width).to(DEV)
+    k = torch.empty((1, new, heads, dim), dtype=dtype, device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(93))
+    first = torch.tensor([5], dtype=torch.int32, device=DEV)
+    gs.mx4_cache_append(cache, table, first, k, k)
+    for at in (0, 1, new // 2 - 7, new - 33):
+        want = gs.mx4_dequantize(gs.mx4_quantize(k[:, at:at + 33].contiguous()), out_dtype=dtype)
+        for got in gs.mx4_cache_read(cache, table, first + at, 33, out_dtype=dtype):
+            assert torch.equal(got, want)
+    if new < 10000:
+        for got in gs.mx4_cache_read(cache, table, first, new, out_dtype=dtype):
+            assert torch.equal(got, gs.mx4_dequantize(gs.mx4_quantize(k), out_dtype=dtype))
 
 
 def test_append_drops_what_has_no_place():
