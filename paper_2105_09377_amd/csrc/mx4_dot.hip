@@ -233,6 +233,46 @@ struct DotPlan {
 };
 int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * ceil_div(N, bn); }
 
+// Tiles of bfloat16 rows with MX4 weights: what a slab of 128 of K takes a workgroup that has a compute unit for itself, and each of several
+// that share one or follow each other on it (us).
+struct WeightWay {
+  DotWay way;
+  int bm, bn;
+  double alone, several;
+};
+constexpr WeightWay kWeightWays[] = {{kWeight32x128, 32, 128, 0.46, 0.43}, {kWeight64x64, 64, 64, 0.47, 0.43}, {kWeight64x128, 64, 128, 0.88, 0.58},
+                                     {kWeight128x128, 128, 128, 1.15, 1.15}, {kWeight128x256, 128, 256, 1.72, 1.75}};
+struct WeightChoice {
+  DotWay way;
+  int splits;
+};
+// The tile, and how many workgroups share one's sum over K (eight slabs each at least), by the time that they should take: the slabs of the
+// busiest compute unit, or what all tiles read at 10 TB/s (200 x 4096 x 11000 in 256 64x64 tiles: 456 MB, 51 us), and where sums are shared 3 us
+// for the second launch and the parts written and read, 8 bytes each at 4 TB/s.  Times that it chooses between, measured: 100 x 8192 x 8192 34.6 in 64x64 tiles, 29.6 in 64x128 by fours, 29.4 in 128x128 by fours; 200 x 8192 x 8192 53.4 in
+// 64x128, 47.4 by twos, 44.2 in 128x256 by fours; 100 x 5000 x 4104 16.9 in 64x64, 20.2 by twos; 256 x 5000 x 4104 28.6 in 64x128, 25.2 by
+// threes; 300 x 11000 x 4096 62.9 in 128x128 by twos, 53.5 in 64x64, 37.5 in 64x128; 20 x 16384 x 1024 7.0 in 32x128, 9.3 by twos; 17 x 8192 x 8192 in
+// 32x128 25.8, 17.7, 13.7 and 15.3 alone, by twos, fours and eights; 2048 x 4096 x 4096 62.8 in 128x256, 73.9 in 128x128.
+WeightChoice weight_choice(int64_t M, int64_t N, int64_t K) {
+  const int64_t slabs = ceil_div(K, 128);
+  WeightChoice best = {kWeight64x64, 1};
+  double least = 1e30;
+  for (const WeightWay& w : kWeightWays) {
+    const int64_t count = tiles(M, N, w.bm, w.bn);
+    for (int n = 1; n <= 16 && (n == 1 || slabs / n >= 8); ++n) {
+      const int64_t on_one = ceil_div(count * n, 256);
+      double t = double(ceil_div(slabs, n)) * (on_one == 1 ? w.alone : w.several * double(on_one));
+      const double read = double(count) * double(slabs) * (w.bm * 256 + w.bn * 68) / 1e7;
+      t = t > read ? t : read;
+      if (n > 1) t += 3.0 + 0.2 * n + double(n) * double(M) * double(N) * 8.0 / 4e6;
+      if (t < least) {
+        least = t;
+        best = {w.way, n};
+      }
+    }
+  }
+  return best;
+}
+
 DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
   DotPlan p = {kRows1, 1, 0, false, 0, 0};
   // Up to 16 rows w is read once by the rows kernel.  Two blocks of 16 columns per wave where that leaves a workgroup for every
@@ -258,25 +298,11 @@ DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
   p.pad = K % 8 != 0;
   p.ldx = round_up(K, 8);
   if (p.pad) p.pad_bytes = size_t(round_up(M * p.ldx * 2, 256));
-  int64_t count = 0;
-  // 2048 x 4096 x 4096 (256 tiles of 128x256) 62.8, 73.9 in 128x128; 512 x 8192 x 8192 (128 of 128x256, 256 of 128x128) 88.8, 68.4,
-  // and 75 in 64x128, 102 in 64x64.
-  if (tiles(M, N, 128, 256) >= 180) p.way = kWeight128x256;
-  else if (t128 >= 160) p.way = kWeight128x128;
-  else if (M <= 32) p.way = kWeight32x128, count = tiles(M, N, 32, 128);
-  else if (t64 > 320) p.way = kWeight64x128;
-  else p.way = kWeight64x64, count = t64;
-  // Fewer tiles than compute units: as many workgroups per tile as fill them, with four slabs each at least (17 x 8192 x 8192 25.8
-  // alone, 17.7, 13.7 and 15.3 by twos, fours and eights; 64 x 8192 x 8192 28.0, 19.9, 20.4, 23.7).
-  if (count > 0 && count < 160) {
-    int64_t splits = (256 + count / 2) / count;
-    const int64_t slabs = ceil_div(K, 128);
-    splits = splits < slabs / 4 ? splits : slabs / 4;
-    splits = splits < 16 ? splits : 16;
-    if (splits > 1) {
-      p.splits = int(splits);
-      p.part_bytes = size_t(splits) * size_t(M) * size_t(N) * 4;
-    }
+  const WeightChoice c = weight_choice(M, N, K);
+  p.way = c.way;
+  if (c.splits > 1) {
+    p.splits = c.splits;
+    p.part_bytes = size_t(c.splits) * size_t(M) * size_t(N) * 4;
   }
   return p;
 }
