@@ -154,7 +154,8 @@ PRODUCTS = [(1, 1, 1), (1, 16, 32), (3, 5, 31), (16, 16, 33), (17, 33, 100), (33
 LARGE = [(3500, 3400, 300), (3400, 3500, 480), (3300, 3600, 512), (2100, 2100, 200), (2050, 2200, 993), (1800, 1800, 700), (1700, 1900, 4400),
          (1030, 1500, 1531), (1030, 1500, 768), (70, 4000, 8192), (128, 2000, 2049)]
 LARGE_WEIGHTS = [(2300, 2600, 200), (2300, 2600, 201), (1700, 1700, 136), (1700, 1700, 1033), (700, 2200, 300), (700, 2200, 65), (20, 3000, 8000),
-                 (32, 700, 7003), (100, 1500, 7000), (50, 2000, 7001), (300, 1000, 2048), (64, 4000, 1000), (129, 5000, 500), (100, 5000, 6200), (257, 3000, 2100), (200, 4100, 1025)]
+                 (32, 700, 7003), (100, 1500, 7000), (50, 2000, 7001), (300, 1000, 2048), (64, 4000, 1000), (129, 5000, 500), (100, 5000, 6200), (257, 3000, 2100), (200, 4100, 1025), (381, 5417, 29), (33, 3241, 5265),
+                 (35, 5974, 8151), (194, 5483, 4485), (300, 11000, 200)]
 
 
 def operands(m, n, k, seed):
