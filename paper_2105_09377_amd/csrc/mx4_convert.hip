@@ -27,7 +27,7 @@ __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_
   if (left >= N) {
     if constexpr (DT == GS_BF16) {
       static_assert(N == 8, "16 bytes");
-      const i32x4 v = *reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at);
+      const i32x4 v = __builtin_nontemporal_load(reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[2 * i] = __uint_as_float(uint32_t(v[i]) << 16);
@@ -36,7 +36,7 @@ __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_
     } else {
 #pragma unroll
       for (int h = 0; h < N / 4; ++h) {
-        const f32x4_any v = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h);
+        const f32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h));
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * h + i] = v[i];
       }
@@ -54,7 +54,7 @@ __device__ __forceinline__ void store_numbers(void* row, int64_t at, int64_t lef
     uint16_t* dst = static_cast<uint16_t*>(row) + at;
     const i32x4 v = mx4_decode8(w, scale);
     if (left >= 8) {
-      *reinterpret_cast<i32x4_any2*>(dst) = v;
+      __builtin_nontemporal_store((i32x4_any2)v, reinterpret_cast<i32x4_any2*>(dst));
     } else {
 #pragma unroll
       for (int i = 0; i < 7; ++i)
@@ -71,7 +71,7 @@ __device__ __forceinline__ void store_numbers(void* row, int64_t at, int64_t lef
     }
     if (left >= N) {
 #pragma unroll
-      for (int h = 0; h < N / 4; ++h) *reinterpret_cast<f32x4_any*>(dst + 4 * h) = f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+      for (int h = 0; h < N / 4; ++h) __builtin_nontemporal_store((f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]}), reinterpret_cast<f32x4_any*>(dst + 4 * h));
     } else {
 #pragma unroll
       for (int i = 0; i < N - 1; ++i)
@@ -98,23 +98,40 @@ __device__ __forceinline__ uint32_t block_scale_byte(const float (&x)[N]) {
 }
 
 // Pieces of 16 bytes of all rows' numbers, one after the other: a workgroup takes 256 P of them, a lane P that lie 256 apart, whose loads are
-// all under way before the first is used.  Rows and places in them come from a division by multiplication where all pieces count in 31
-// bits (BIG: 64-bit divisions).
+// all under way before the first is used.  What pieces cost in instructions counts (16384 x 8190 floats read back with 64-bit places 118 us):
+// rows and places are counted in 32 bits where all numbers do (BIG: in 64), the first of a lane's from a division by multiplication, the others
+// from it.
 template <int DT>
 constexpr int kNumbers = DT == GS_BF16 ? 8 : 4;
 template <bool BIG>
 struct Pieces {
-  int64_t per_row, total;
+  using Index = std::conditional_t<BIG, int64_t, uint32_t>;
+  Index per_row, total;
   FastDiv by_row;
-  __device__ void place(int64_t at, int64_t* row, int64_t* piece) const {
+  // of pieces at, at + 256 ..; those behind the last are the first
+  template <int P>
+  __device__ void places(Index at, Index (&row)[P], Index (&piece)[P]) const {
+    divide(at < total ? at : 0, &row[0], &piece[0]);
+    const bool wide = per_row >= kThreads;               // (uniform)
+#pragma unroll
+    for (int p = 1; p < P; ++p) {
+      if (wide) {
+        const Index next = piece[p - 1] + kThreads;
+        const bool same = next < per_row;
+        row[p] = same ? row[p - 1] : row[p - 1] + 1;
+        piece[p] = same ? next : next - per_row;
+      } else {
+        divide(at + p * kThreads < total ? at + p * kThreads : 0, &row[p], &piece[p]);
+      }
+      if (at + p * kThreads >= total) row[p] = piece[p] = 0;
+    }
+  }
+  __device__ void divide(Index at, Index* row, Index* piece) const {
     if constexpr (BIG) {
       *row = at / per_row;
       *piece = at - *row * per_row;
     } else {
-      uint32_t q, r;
-      by_row.divmod(uint32_t(at), &q, &r);
-      *row = q;
-      *piece = r;
+      by_row.divmod(at, row, piece);
     }
   }
 };
@@ -122,29 +139,28 @@ struct Pieces {
 // A row's pieces are counted up to whole runs of scale bytes, the padding written as zeros by the same lanes.
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  using Index = typename Pieces<BIG>::Index;
   constexpr int N = kNumbers<DT>;
-  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
-  int64_t row[P], piece[P];
+  const Index cols = Index(a.cols), blocks = Index(mx4_blocks(a.cols)), pitch = Index(mx4_scale_pitch(a.cols));
+  const Index base = Index(blockIdx.x) * (kThreads * P) + threadIdx.x;
+  Index row[P], piece[P];
   float x[P][N];
+  n.places(base, row, piece);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int64_t at = base + p * kThreads;
-    const bool there = at < n.total;
-    n.place(there ? at : 0, &row[p], &piece[p]);
-    if (!there) row[p] = -1;
-    const void* const src = static_cast<const uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
-    load_numbers<DT, N>(src, piece[p] * N, there ? a.cols - piece[p] * N : 0, x[p]);
+    const Index at = piece[p] * N;
+    load_numbers<DT, N>(a.plain, int64_t(row[p] * cols + at), at + N <= cols ? N : at < cols ? int(cols - at) : 0, x[p]);
   }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const uint32_t byte = block_scale_byte<N>(x[p]);
-    if (row[p] < 0) continue;
-    const int64_t block = piece[p] / (kMx4Block / N);
+    if (base + p * kThreads >= n.total) continue;
+    const Index block = piece[p] / (kMx4Block / N);
     if (block < blocks) {
       float eight[8] = {};
 #pragma unroll
       for (int i = 0; i < N; ++i) eight[i] = x[p][i];
-      const int64_t to = row[p] * blocks * (kMx4Block / N) + piece[p];
+      const Index to = row[p] * blocks * (kMx4Block / N) + piece[p];
       if constexpr (N == 8) static_cast<uint32_t*>(a.values)[to] = mx4_encode8(eight, byte);
       else static_cast<uint16_t*>(a.values)[to] = uint16_t(mx4_encode8(eight, byte));
     }
@@ -154,15 +170,16 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4ConvertArgs a
 
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  using Index = typename Pieces<BIG>::Index;
   constexpr int N = kNumbers<DT>;
-  const int64_t blocks = mx4_blocks(a.cols), pitch = mx4_scale_pitch(a.cols), base = int64_t(blockIdx.x) * (kThreads * P) + threadIdx.x;
-  int64_t row[P], piece[P];
+  const Index cols = Index(a.cols), blocks = Index(mx4_blocks(a.cols)), pitch = Index(mx4_scale_pitch(a.cols));
+  const Index base = Index(blockIdx.x) * (kThreads * P) + threadIdx.x;
+  Index row[P], piece[P];
   uint32_t w[P], byte[P];
+  n.places(base, row, piece);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int64_t at = base + p * kThreads;
-    n.place(at < n.total ? at : 0, &row[p], &piece[p]);
-    const int64_t from = row[p] * blocks * (kMx4Block / N) + piece[p];
+    const Index from = row[p] * blocks * (kMx4Block / N) + piece[p];
     if constexpr (N == 8) w[p] = static_cast<const uint32_t*>(a.values)[from];
     else w[p] = static_cast<const uint16_t*>(a.values)[from];
     byte[p] = static_cast<const uint8_t*>(a.scales)[row[p] * pitch + piece[p] / (kMx4Block / N)];
@@ -170,28 +187,108 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4ConvertArgs
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (base + p * kThreads >= n.total) continue;
-    void* const dst = static_cast<uint8_t*>(a.plain) + row[p] * a.cols * int64_t(dtype_size(DT));
-    store_numbers<DT, N>(dst, piece[p] * N, a.cols - piece[p] * N, w[p], mx4_scale(byte[p]));
+    const Index at = piece[p] * N;
+    store_numbers<DT, N>(a.plain, int64_t(row[p] * cols + at), at + N <= cols ? N : int(cols - at), w[p], mx4_scale(byte[p]));
   }
 }
 
+// Back into rows that do not all begin on 16 bytes: pieces are those of the result's memory, so that whole lines are written.  A piece may have
+// numbers of two blocks; one with numbers of two rows is written number by number.  There are cols >= N numbers in a row, n.per_row of them.
 template <int DT, int P, bool BIG>
-hipError_t launch_convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
-  const int64_t total = a.rows * per_row, groups = ceil_div(total, kThreads * P);
+__global__ void __launch_bounds__(kThreads) mx4_dequantize_flat_kernel(Mx4ConvertArgs a, Pieces<BIG> n) {
+  using Index = typename Pieces<BIG>::Index;
+  constexpr int N = kNumbers<DT>;
+  typedef uint32_t u32_any __attribute__((aligned(1)));
+  typedef uint64_t u64_any __attribute__((aligned(1)));
+  using Codes = std::conditional_t<N == 8, uint64_t, uint32_t>;
+  using CodesAny = std::conditional_t<N == 8, u64_any, u32_any>;
+  const Index cols = n.per_row, blocks = Index(mx4_blocks(a.cols)), pitch = Index(mx4_scale_pitch(a.cols)), most = blocks * 16 - sizeof(Codes);
+  const Index base = (Index(blockIdx.x) * (kThreads * P) + threadIdx.x) * N;
+  const uint8_t *const values = static_cast<const uint8_t*>(a.values), *const scales = static_cast<const uint8_t*>(a.scales);
+  Index row[P], first[P];             // of the piece's first number
+  uint32_t w[P], byte[P][2];
+  int border[P];                      // numbers from here on are of the second block
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    n.divide(base + p * (kThreads * N) < n.total ? base + p * (kThreads * N) : 0, &row[p], &first[p]);
+    const Index at = first[p] / 2 < most ? first[p] / 2 : most, last = first[p] + N <= cols ? first[p] + N - 1 : cols - 1;
+    const Codes c = *reinterpret_cast<const CodesAny*>(values + (row[p] * blocks * 16 + at));
+    w[p] = uint32_t(c >> (int(first[p] - 2 * at) * 4));
+    byte[p][0] = scales[row[p] * pitch + first[p] / kMx4Block];
+    byte[p][1] = scales[row[p] * pitch + last / kMx4Block];
+    border[p] = int(last / kMx4Block * kMx4Block) - int(first[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const Index number = base + p * (kThreads * N);
+    if (number >= n.total) continue;
+    if (first[p] + N > cols) {
+#pragma unroll 1
+      for (int i = 0; i < N && number + i < n.total; ++i) {
+        const bool wraps = first[p] + i >= cols;
+        const Index r = wraps ? row[p] + 1 : row[p], c = wraps ? first[p] + i - cols : first[p] + i;
+        float pair[2];
+        mx4_decode2_f32<0>(values[r * blocks * 16 + c / 2], mx4_scale(scales[r * pitch + c / kMx4Block]), pair);
+        const float v = c % 2 ? pair[1] : pair[0];
+        if constexpr (DT == GS_BF16) static_cast<uint16_t*>(a.plain)[number + i] = float_to_bf16_bits(v);
+        else static_cast<float*>(a.plain)[number + i] = v;
+      }
+      continue;
+    }
+    const float s0 = mx4_scale(byte[p][0]), s1 = mx4_scale(byte[p][1]);
+    if constexpr (DT == GS_BF16) {
+      const i32x4 x0 = mx4_decode8(w[p], s0), x1 = mx4_decode8(w[p], s1);
+      i32x4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t low = uint32_t(2 * i < border[p] ? x0[i] : x1[i]) & 0xffffu, high = uint32_t(2 * i + 1 < border[p] ? x0[i] : x1[i]) & 0xffff0000u;
+        x[i] = int32_t(low | high);
+      }
+      __builtin_nontemporal_store(x, reinterpret_cast<i32x4*>(static_cast<uint16_t*>(a.plain) + number));
+    } else {
+      float x0[4], x1[4];
+      mx4_decode2_f32<0>(w[p], s0, x0);
+      mx4_decode2_f32<1>(w[p], s0, x0 + 2);
+      mx4_decode2_f32<0>(w[p], s1, x1);
+      mx4_decode2_f32<1>(w[p], s1, x1 + 2);
+      f32x4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = i < border[p] ? x0[i] : x1[i];
+      __builtin_nontemporal_store(x, reinterpret_cast<f32x4*>(static_cast<float*>(a.plain) + number));
+    }
+  }
+}
+
+enum Convert { kQuantize, kDequantize, kDequantizeFlat };
+template <int DT, int P, bool BIG>
+hipError_t launch_convert(const Mx4ConvertArgs& a, int64_t per_row, Convert what, hipStream_t s) {
+  // (the flat kernel counts numbers, the others pieces)
+  const bool flat = what == kDequantizeFlat;
+  const int64_t total = flat ? a.rows * a.cols : a.rows * per_row, step = flat ? a.cols : per_row;
+  const int64_t groups = ceil_div(total, kThreads * P * (flat ? kNumbers<DT> : 1));
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  const Pieces<BIG> n{per_row, total, FastDiv::make(BIG ? 1u : uint32_t(per_row))};
-  if (quantize) hipLaunchKernelGGL((mx4_quantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n);
-  else hipLaunchKernelGGL((mx4_dequantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n);
+  using Index = typename Pieces<BIG>::Index;
+  const Pieces<BIG> n{Index(step), Index(total), FastDiv::make(BIG ? 1u : uint32_t(step))};
+  const dim3 grid{unsigned(groups)}, block(kThreads);
+  if (what == kQuantize) hipLaunchKernelGGL((mx4_quantize_kernel<DT, P, BIG>), grid, block, 0, s, a, n);
+  else if (what == kDequantize) hipLaunchKernelGGL((mx4_dequantize_kernel<DT, P, BIG>), grid, block, 0, s, a, n);
+  else hipLaunchKernelGGL((mx4_dequantize_flat_kernel<DT, P, BIG>), grid, block, 0, s, a, n);
   return hipGetLastError();
 }
 // Four pieces per lane where that still leaves eight workgroups for every compute unit.
 template <int DT>
-hipError_t convert(const Mx4ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
+hipError_t convert(const Mx4ConvertArgs& a, int64_t per_row, Convert what, hipStream_t s) {
   const int64_t total = a.rows * per_row;
   if (total == 0) return hipSuccess;
-  if (total > 0x7fffffff) return launch_convert<DT, 4, true>(a, per_row, quantize, s);
-  if (total >= int64_t(256) * 8 * 4 * kThreads) return launch_convert<DT, 4, false>(a, per_row, quantize, s);
-  return launch_convert<DT, 1, false>(a, per_row, quantize, s);
+  if (total > (int64_t(1) << 30) / kNumbers<DT>) return launch_convert<DT, 4, true>(a, per_row, what, s);
+  if (total >= int64_t(256) * 8 * 4 * kThreads) return launch_convert<DT, 4, false>(a, per_row, what, s);
+  return launch_convert<DT, 1, false>(a, per_row, what, s);
+}
+// Rows of 16384 x 8190 floats, which begin on 8 bytes: 89 us, and 120 with pieces that begin where the rows do.
+template <int DT>
+hipError_t dequantize(const Mx4ConvertArgs& a, hipStream_t s) {
+  constexpr int N = kNumbers<DT>;
+  return convert<DT>(a, ceil_div(a.cols, N), a.cols % N == 0 || a.rows <= 1 || a.cols < 128 ? kDequantize : kDequantizeFlat, s);
 }
 
 // Tokens of a cache.  A token's place takes two loads, one behind the other (its sequence's first position, an entry of the table), so a lane has
@@ -374,11 +471,11 @@ hipError_t launch_tokens(const Mx4TokenArgs& a, hipStream_t s) {
 
 hipError_t launch_mx4_quantize(const Mx4ConvertArgs& a, hipStream_t s) {
   const int64_t per_row = mx4_scale_pitch(a.cols) * kMx4Block;
-  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row / 8, true, s) : convert<GS_F32>(a, per_row / 4, true, s);
+  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row / 8, kQuantize, s) : convert<GS_F32>(a, per_row / 4, kQuantize, s);
 }
 
 hipError_t launch_mx4_dequantize(const Mx4ConvertArgs& a, hipStream_t s) {
-  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, ceil_div(a.cols, 8), false, s) : convert<GS_F32>(a, ceil_div(a.cols, 4), false, s);
+  return a.dtype == GS_BF16 ? dequantize<GS_BF16>(a, s) : dequantize<GS_F32>(a, s);
 }
 
 hipError_t launch_mx4_append(const Mx4TokenArgs& a, hipStream_t s) { return launch_tokens<true>(a, s); }

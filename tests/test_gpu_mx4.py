@@ -118,6 +118,23 @@ def test_conversions_of_large_matrices(rows, cols, dtype):
     same_values(gs.mx4_dequantize(m, out_dtype=dtype), mx4.dequantize(packed, scales, cols))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("offset", [0, 8])
+def test_dequantize_into_rows_anywhere(offset, dtype):
+    """Rows that begin and end anywhere in a line: nothing around the result is written."""
+    for rows, cols in ((1, 1), (1, 7), (3, 2), (5, 31), (4, 33), (7, 63), (6, 64), (3, 97), (9, 130), (2, 1025), (5, 129), (11, 163), (40, 223)):
+        x = normal((rows, cols), 95 + cols, dtype, spread=3.0)
+        x[rows // 2, 0] = float("nan")
+        packed, scales = mx4.quantize(to_oracle(x))
+        m = gs.mx4_quantize(x.to(DEV))
+        for odt in (BF, F32):
+            around = torch.full((rows * cols + 64,), 7.0, dtype=odt, device=DEV)
+            inner = around[16 + offset:16 + offset + rows * cols].view(rows, cols)
+            gs.mx4_dequantize(m, out=inner)
+            same_values(inner, mx4.dequantize(packed, scales, cols))
+            assert (around[:16 + offset] == 7).all() and (around[16 + offset + rows * cols:] == 7).all()
+
+
 def test_conversions_beyond_32_bits():
     """More than 2^31 pieces of numbers: the same as row by row."""
     rows, cols = 70000, 131075
