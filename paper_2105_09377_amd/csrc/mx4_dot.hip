@@ -288,8 +288,9 @@ DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
     // 4096 cubed (256 tiles of 256x256) 39 in those, 47 in 128x128 and 71 in 64x64 tiles; 2048 cubed (64 of them, 256 of 128x128)
     // 17, 9.7 and 11.3; 1021 x 2000 x 1531 (128 of 128x128) 7.1 and 6.0.  Tiles that a compute unit has for itself are paid for
     // in latency: more slabs under way (64 x 8192 x 8192 11.3 with four, 18.4 with two), or, where those are few, more waves (2048
-    // cubed 9.7 with eight waves, 10.5 with four; 512 x 8192 x 8192 27.8 and 26.3).
-    if (tiles(M, N, 256, 256) >= 180) p.way = kTile256x256;
+    // cubed 9.7 with eight waves, 10.5 with four; 512 x 8192 x 8192 27.8 and 26.3).  More 128x128 tiles than the chip has at a time, two
+    // to a compute unit, are slower than fewer large ones (3000 cubed, 576 of them and 144 of 256x256, 32.4 and 25.6).
+    if (tiles(M, N, 256, 256) >= 180 || t128 > 512) p.way = kTile256x256;
     else if (t128 > 256) p.way = kTile128x128;
     else if (t128 >= 192) p.way = K > 16 * 256 ? kTile128x128Long : kTile128x128Few;
     else p.way = t64 <= 256 ? kTile64x64Few : kTile64x64;

@@ -70,7 +70,7 @@ __device__ __forceinline__ void mx4_write_back(const Mx4DotArgs& a, f32x16 (&acc
       if (n + 8 <= a.N) {
         if (a.out_dtype == GS_BF16) {
           const i32x4 w = {int32_t(pack_bf16x2(x[0], x[1])), int32_t(pack_bf16x2(x[2], x[3])), int32_t(pack_bf16x2(x[4], x[5])), int32_t(pack_bf16x2(x[6], x[7]))};
-          *reinterpret_cast<i32x4_any2t*>(static_cast<uint16_t*>(a.out) + at) = w;
+          __builtin_nontemporal_store((i32x4_any2t)w, reinterpret_cast<i32x4_any2t*>(static_cast<uint16_t*>(a.out) + at));
         } else {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
