@@ -31,9 +31,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 32, NJ = WN / 32;
   static_assert(BM % (4 * NW) == 0 && BN % 16 == 0 && NW % 4 == 0, "whole transfers");
   constexpr int XQ = BM / 4 / NW;                                  // transfers of x per wave and slab: 4 rows each
-  constexpr int kWAll = BN / 16, WQ = (kWAll + NW - 1) / NW;       // of codes: 16 rows each
-  constexpr int kSAll = (BN + 63) / 64, SQ = (kSAll + NW - 1) / NW;    // of scales: 64 rows each
-  constexpr int Q = XQ + WQ + SQ;                                  // (some are made twice, so that every wave counts the same number)
+  constexpr int kWAll = BN / 16, WQ = kWAll / NW;                  // of codes: 16 rows each
+  constexpr int kSAll = (BN + 63) / 64;                            // of scales: 64 rows each, in lines of their own, by the first waves
+  static_assert(kSAll <= NW && kWAll % NW == 0, "one of scales at most, codes dealt evenly");
+  constexpr int Q = XQ + WQ;                                       // of every wave; one more of the first kSAll
   constexpr int kX = BM * 256, kW = BN * 64, kBuf = kX + kW + kSAll * 256;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
 
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
   const int32_t m_last = int32_t(a.M - m0 < BM ? a.M - m0 : BM) - 1, n_last = int32_t(a.N - n0 < BN ? a.N - n0 : BN) - 1;
   const int xcol = (lane & 15) ^ (4 * (wave & 3) + lane / 16);     // row % 16 = 4 (transfer % 4) + lane / 16
   const int wcol = (lane & 3) ^ ((lane / 16) & 3);                 // row / 4 % 4
-  uint32_t xo[XQ], wo[WQ], so[SQ];
+  uint32_t xo[XQ], wo[WQ];
 #pragma unroll
   for (int q = 0; q < XQ; ++q) {
     const int32_t row = (wave + q * NW) * 4 + lane / 16;
@@ -62,14 +63,12 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
   }
 #pragma unroll
   for (int q = 0; q < WQ; ++q) {
-    const int32_t row = (wave + q * NW) % kWAll * 16 + lane / 4;
+    const int32_t row = (wave + q * NW) * 16 + lane / 4;
     wo[q] = uint32_t(row < n_last ? row : n_last) * uint32_t(nb * 16) + uint32_t(wcol * 16);
   }
-#pragma unroll
-  for (int q = 0; q < SQ; ++q) {
-    const int32_t row = (wave + q * NW) % kSAll * 64 + lane;
-    so[q] = uint32_t(row < n_last ? row : n_last) * uint32_t(pitch);
-  }
+  const bool has_scales = wave < kSAll;
+  const int32_t scale_row = wave * 64 + lane;
+  const uint32_t so = uint32_t(scale_row < n_last ? scale_row : n_last) * uint32_t(pitch);
   const uint32_t x_fix = xcol >= x_tail ? uint32_t(xcol * 16) : 0u, w_fix = wcol >= w_tail ? uint32_t(wcol * 16) : 0u;
 
   const uint32_t lds0 = lds_addr_of(lds);
@@ -79,8 +78,13 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
     const uint32_t base = lds0 + uint32_t(buf) * kBuf;
     if constexpr (i < XQ) lds_dma16_off(xb + int64_t(slab) * 256, xo[i] - (last ? x_fix : 0u), base + (wave + i * NW) * 1024);
     else if constexpr (i < XQ + WQ)
-      lds_dma16_off(wb + int64_t(slab) * 64, wo[i - XQ] - (last ? w_fix : 0u), base + kX + (wave + (i - XQ) * NW) % kWAll * 1024);
-    else lds_dma4_off(sb + int64_t(slab) * 4, so[i - XQ - WQ], base + kX + kW + (wave + (i - XQ - WQ) * NW) % kSAll * 256);
+      lds_dma16_off(wb + int64_t(slab) * 64, wo[i - XQ] - (last ? w_fix : 0u), base + kX + (wave + (i - XQ) * NW) * 1024);
+    else if (has_scales) lds_dma4_off(sb + int64_t(slab) * 4, so, base + kX + kW + wave * 256);
+  };
+  auto wait_slabs = [&](auto slabs_) {                             // until at most so many slabs' transfers are under way
+    constexpr int slabs = decltype(slabs_)::value;
+    if (has_scales) wait_vmem<slabs*(Q + 1)>();
+    else wait_vmem<slabs * Q>();
   };
 
   f32x16 acc[MI][NJ];
@@ -141,7 +145,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
       decode(std::integral_constant<int, step + 1>{}, std::integral_constant<int, set ^ 1>{});
       static_for<MI * NJ>([&](auto i_) { products(std::integral_constant<int, set>{}, i_); });
     });
-    if constexpr (ISSUE) wait_vmem<(NS - 2) * Q>();
+    if constexpr (ISSUE) wait_slabs(std::integral_constant<int, NS - 2>{});
     else wait_vmem<0>();
     lds_barrier_tracked();
     const int done = buf;
@@ -149,10 +153,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
     read_w(lds + buf * kBuf);
     read_x(lds + buf * kBuf, I0{}, I0{});
     __builtin_amdgcn_sched_barrier(0);
-    static_for<(MI * NJ > (ISSUE ? Q : 0) ? MI * NJ : Q)>([&](auto i_) {
+    static_for<(MI * NJ > (ISSUE ? Q + 1 : 0) ? MI * NJ : Q + 1)>([&](auto i_) {
       constexpr int i = decltype(i_)::value;
       if constexpr (i < MI * NJ) products(I1{}, i_);
-      if constexpr (ISSUE && i < Q) issue_one(s + NS, done, i_);
+      if constexpr (ISSUE && i <= Q) issue_one(s + NS, done, i_);
       __builtin_amdgcn_sched_barrier(0);
     });
     scales();
@@ -162,10 +166,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64) mx4_weight_tile_kernel(Mx4DotA
 
   static_for<NS>([&](auto b_) {
     constexpr int b = decltype(b_)::value;
-    if (s + b < mine.end) static_for<Q>([&](auto i_) { issue_one(s + b, b, i_); });
+    if (s + b < mine.end) static_for<Q + 1>([&](auto i_) { issue_one(s + b, b, i_); });
   });
   asm volatile("" ::"s"(a.relu), "s"(a.M), "s"(a.N), "s"(a.out), "s"(a.out_dtype));   // not in the loop: scalar loads share a counter with LDS
-  if (s + NS <= mine.end) wait_vmem<(NS - 1) * Q>();
+  if (s + NS <= mine.end) wait_slabs(std::integral_constant<int, NS - 1>{});
   else wait_vmem<0>();
   lds_barrier_tracked();
   read_w(lds);
