@@ -132,6 +132,7 @@ struct Mx4AttendArgs {
   int32_t queries, group;
   int32_t parts, tiles;   // set by the launcher: workgroups along a sequence; 16-row tiles of a workgroup;
   int32_t least;          // 64-token tiles of a part
+  FastDiv by_group, by_rows, by_heads, by_parts;      // rows: queries * group
   int32_t slots;          // parts of all sequences together where they are cut to the same length, else 0
 };
 hipError_t launch_mx4_attend(const Mx4AttendArgs& a, hipStream_t s);

@@ -453,8 +453,8 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
   const int32_t at = SPLIT ? int32_t(blockIdx.x) : int32_t(blockIdx.x) * G + group;
   const int32_t rows = a.queries * a.group, row_tiles = (rows + kRows - 1) / kRows;
   const bool ok = at < total_rows && (SPLIT || group < G);
-  const int32_t bh = ok ? at / rows : 0, row = ok ? at - bh * rows : 0, row_tile = row / kRows;
-  const int32_t b = bh / a.cache.heads, head = bh - b * a.cache.heads;
+  const int32_t bh = ok ? int32_t(a.by_rows.div(uint32_t(at))) : 0, row = ok ? at - bh * rows : 0, row_tile = row / kRows;
+  const int32_t b = int32_t(a.by_heads.div(uint32_t(bh))), head = bh - b * a.cache.heads;
   const int32_t row0 = row_tile * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
   Cut cut;
   if (a.slots) {                     // (all lanes of a wave take part)
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
     }
   }
   const float inv = total != 0.0f ? 1.0f / total : 0.0f;
-  const int32_t i = row / a.group, h = row - i * a.group;
+  const int32_t i = int32_t(a.by_group.div(uint32_t(row))), h = row - i * a.group;
   const int64_t dst = ((int64_t(b) * a.queries + i) * a.cache.heads * a.group + int64_t(head) * a.group + h) * D + d;
   if (a.out_dtype == GS_BF16)
     *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + dst) = i32x2{int32_t(pack_bf16x2(x[0] * inv, x[1] * inv)), int32_t(pack_bf16x2(x[2] * inv, x[3] * inv))};
@@ -609,6 +609,10 @@ hipError_t launch_mx4_attend(const Mx4AttendArgs& given, hipStream_t s) {
   Mx4AttendArgs a = given;
   plan(&a);
   if (a.batch == 0 || a.queries == 0 || a.group == 0) return hipSuccess;
+  a.by_group = FastDiv::make(uint32_t(a.group));
+  a.by_rows = FastDiv::make(uint32_t(a.queries) * uint32_t(a.group));
+  a.by_heads = FastDiv::make(uint32_t(a.cache.heads));
+  a.by_parts = FastDiv::make(uint32_t(a.parts));
   switch (a.cache.dim) {
     case 64: return launch_d<64>(a, s);
     case 96: return launch_d<96>(a, s);

@@ -23,7 +23,8 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const Mx4AttendArgs& a, int32_t len, int32_t row0, int32_t row1) {
   Span s;
-  const int32_t first = len - a.queries + row0 / a.group, last = len - a.queries + row1 / a.group;    // positions
+  const int32_t first = len - a.queries + int32_t(a.by_group.div(uint32_t(row0))),
+                last = len - a.queries + int32_t(a.by_group.div(uint32_t(row1)));    // positions
   s.hi = last + 1 > 0 ? last + 1 : 0;
   int32_t lo = 0;
   if (a.window > 0 && first >= a.window) lo = first - int32_t(a.window) + 1;
@@ -43,7 +44,7 @@ struct Cut {
 // Every task (sequence, cache head, row tile) into as many parts, `least` tiles long at least.
 __device__ __forceinline__ Cut cut_alike(const Mx4AttendArgs& a, int32_t total, int64_t task) {
   Cut c;
-  c.per = (total + a.parts - 1) / a.parts;
+  c.per = int32_t(a.by_parts.div(uint32_t(total + a.parts - 1)));
   c.per = c.per > a.least ? c.per : a.least;
   c.parts = total > c.per ? (total + c.per - 1) / c.per : 1;
   c.base = task * a.parts;
