@@ -115,8 +115,19 @@ struct Mx4DotArgs {       // out[m][n] = sum_k x[m][k] w[n][k]
   int32_t splits;         // set by the launcher: workgroups that share the sum over K of a tile; above 1, `out` has as many
                           // results in fp32, one after the other
 };
-hipError_t launch_mx4_dot(const Mx4DotArgs& a, void* workspace, hipStream_t s);
-size_t mx4_dot_workspace(bool x_is_bf16, int64_t M, int64_t N, int64_t K);
+// How a product is done.
+enum Mx4DotWay { kRows1, kRows2, kTile64x64Few, kTile64x64, kTile128x128Few, kTile128x128Long, kTile128x128, kTile256x256,   // two MX4 operands
+                 kWeight32x128, kWeight64x64, kWeight64x128, kWeight128x128, kWeight128x256 };
+struct Mx4DotPlan {
+  Mx4DotWay way;
+  int splits;             // workgroups that share the sum of a tile
+  int64_t ldx;            // bfloat16 x in tiles: numbers between rows
+  bool pad;               // into the workspace first
+  size_t pad_bytes, part_bytes;
+  size_t workspace() const { return pad_bytes + part_bytes; }
+};
+Mx4DotPlan plan_mx4_dot(bool x_is_bf16, int64_t M, int64_t N, int64_t K);
+hipError_t launch_mx4_dot(const Mx4DotArgs& a, const Mx4DotPlan& plan, void* workspace, hipStream_t s);
 
 struct Mx4AttendArgs {
   Mx4CacheShape cache;

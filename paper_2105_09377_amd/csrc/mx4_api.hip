@@ -195,9 +195,10 @@ int run_dot(Mx4DotArgs a, const gs_mx4* a1, gs_ap* out, int act, void* workspace
   a.out = out->data;
   a.out_dtype = out->dtype;
   a.relu = act == GS_ACT_RELU;
-  const size_t need = mx4_dot_workspace(!a.xs, a.M, a.N, a.K);
+  const Mx4DotPlan plan = plan_mx4_dot(!a.xs, a.M, a.N, a.K);
+  const size_t need = plan.workspace();
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return GS_ERR_WORKSPACE;
-  return launch_status(launch_mx4_dot(a, workspace, static_cast<hipStream_t>(stream)));
+  return launch_status(launch_mx4_dot(a, plan, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -246,7 +247,7 @@ int glenside_mx4_dot(const gs_mx4* a0, const gs_mx4* a1, gs_ap* out, int act, vo
 size_t glenside_mx4_dot_workspace(const gs_mx4* a0, const gs_mx4* a1) {
   int64_t M, N, K, K1;
   if (check_mx4(a0, false, &M, &K) || check_mx4(a1, false, &N, &K1) || K != K1) return 0;
-  return mx4_dot_workspace(false, M, N, K);
+  return plan_mx4_dot(false, M, N, K).workspace();
 }
 
 int glenside_mx4_weight_dot(const gs_ap* a0, const gs_mx4* a1, gs_ap* out, int act, void* workspace, size_t workspace_bytes, void* stream) {
@@ -270,7 +271,7 @@ size_t glenside_mx4_weight_dot_workspace(const gs_ap* a0, const gs_mx4* a1) {
   int64_t N, K;
   if (check_ap(a0, false) || check_mx4(a1, false, &N, &K)) return 0;
   if (product(a0->shape + a0->n_access, a0->rank - a0->n_access) != K) return 0;
-  return mx4_dot_workspace(true, product(a0->shape, a0->n_access), N, K);
+  return plan_mx4_dot(true, product(a0->shape, a0->n_access), N, K).workspace();
 }
 
 size_t glenside_mx4_cache_bytes(const gs_mx4_cache* cache) {

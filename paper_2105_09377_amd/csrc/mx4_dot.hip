@@ -221,29 +221,20 @@ __global__ void __launch_bounds__(256) mx4_pad_rows_kernel(const uint16_t* x, ui
   }
 }
 
-// How a product with MX4 weights is done (times in us).
-enum DotWay { kRows1, kRows2, kTile64x64Few, kTile64x64, kTile128x128Few, kTile128x128Long, kTile128x128, kTile256x256,   // two MX4 operands
-              kWeight32x128, kWeight64x64, kWeight64x128, kWeight128x128, kWeight128x256 };
-struct DotPlan {
-  DotWay way;
-  int splits;            // workgroups that share the sum of a tile
-  int64_t ldx;           // bfloat16 x in tiles: numbers between rows
-  bool pad;              // into the workspace first
-  size_t pad_bytes, part_bytes;
-};
+// How a product is done (times in us).
 int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * ceil_div(N, bn); }
 
 // Tiles of bfloat16 rows with MX4 weights: what a slab of 128 of K takes a workgroup that has a compute unit for itself, and each of several
 // that share one or follow each other on it (us).
 struct WeightWay {
-  DotWay way;
+  Mx4DotWay way;
   int bm, bn;
   double alone, several;
 };
 constexpr WeightWay kWeightWays[] = {{kWeight32x128, 32, 128, 0.46, 0.43}, {kWeight64x64, 64, 64, 0.47, 0.43}, {kWeight64x128, 64, 128, 0.88, 0.58},
                                      {kWeight128x128, 128, 128, 1.15, 1.15}, {kWeight128x256, 128, 256, 1.72, 1.75}};
 struct WeightChoice {
-  DotWay way;
+  Mx4DotWay way;
   int splits;
 };
 // The tile, and how many workgroups share one's sum over K (eight slabs each at least), by the time that they should take: the slabs of the
@@ -253,17 +244,18 @@ struct WeightChoice {
 // threes; 300 x 11000 x 4096 62.9 in 128x128 by twos, 53.5 in 64x64, 37.5 in 64x128; 20 x 16384 x 1024 7.0 in 32x128, 9.3 by twos; 17 x 8192 x 8192 in
 // 32x128 25.8, 17.7, 13.7 and 15.3 alone, by twos, fours and eights; 2048 x 4096 x 4096 62.8 in 128x256, 73.9 in 128x128.
 WeightChoice weight_choice(int64_t M, int64_t N, int64_t K) {
-  const int64_t slabs = ceil_div(K, 128);
+  const int32_t slabs = int32_t(ceil_div(K, 128));                 // (K is at most 2^22)
   WeightChoice best = {kWeight64x64, 1};
   double least = 1e30;
   for (const WeightWay& w : kWeightWays) {
     const int64_t count = tiles(M, N, w.bm, w.bn);
-    for (int n = 1; n <= 16 && (n == 1 || slabs / n >= 8); ++n) {
-      const int64_t on_one = ceil_div(count * n, 256);
-      double t = double(ceil_div(slabs, n)) * (on_one == 1 ? w.alone : w.several * double(on_one));
-      const double read = double(count) * double(slabs) * (w.bm * 256 + w.bn * 68) / 1e7;
+    const double read = double(count) * slabs * (w.bm * 256 + w.bn * 68) / 1e7, part = double(M) * double(N) * 8.0 / 4e6;
+    // (more than four workgroups for each compute unit are no help)
+    for (int32_t n = 1; n <= 16 && (n == 1 || (slabs / n >= 8 && count * n <= 1024)); ++n) {
+      const int64_t on_one = (count * n + 255) / 256;
+      double t = double((slabs + n - 1) / n) * (on_one == 1 ? w.alone : w.several * double(on_one));
       t = t > read ? t : read;
-      if (n > 1) t += 3.0 + 0.2 * n + double(n) * double(M) * double(N) * 8.0 / 4e6;
+      if (n > 1) t += 3.0 + 0.2 * n + n * part;
       if (t < least) {
         least = t;
         best = {w.way, n};
@@ -273,8 +265,10 @@ WeightChoice weight_choice(int64_t M, int64_t N, int64_t K) {
   return best;
 }
 
-DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
-  DotPlan p = {kRows1, 1, 0, false, 0, 0};
+}  // namespace
+
+Mx4DotPlan plan_mx4_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
+  Mx4DotPlan p = {kRows1, 1, 0, false, 0, 0};
   // Up to 16 rows w is read once by the rows kernel.  Two blocks of 16 columns per wave where that leaves a workgroup for every
   // compute unit (1 x 8192 x 8192 bf16 10.0 against 11.7 with one; 1 x 4096 x 4096 6.1 against 4.7).  More rows, few tiles: the
   // waves of a workgroup share K, which a tile walks alone (MX4 100 x 700 x 5000 5.3 against 7.4 in 64x64 tiles, 40 x 300 x 16000
@@ -308,17 +302,9 @@ DotPlan plan_dot(bool xbf, int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
-}  // namespace
-
-size_t mx4_dot_workspace(bool x_is_bf16, int64_t M, int64_t N, int64_t K) {
-  const DotPlan p = plan_dot(x_is_bf16, M, N, K);
-  return p.pad_bytes + p.part_bytes;
-}
-
-hipError_t launch_mx4_dot(const Mx4DotArgs& given, void* workspace, hipStream_t s) {
+hipError_t launch_mx4_dot(const Mx4DotArgs& given, const Mx4DotPlan& p, void* workspace, hipStream_t s) {
   Mx4DotArgs a = given;
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  const DotPlan p = plan_dot(!a.xs, a.M, a.N, a.K);
   if (p.pad) {
     const int64_t pieces = a.M * (p.ldx / 8), groups = ceil_div(pieces, 256);
     hipLaunchKernelGGL(mx4_pad_rows_kernel, dim3(unsigned(groups < 4096 ? groups : 4096)), dim3(256), 0, s, static_cast<const uint16_t*>(a.x),
