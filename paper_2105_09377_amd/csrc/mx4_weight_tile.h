@@ -9,7 +9,8 @@
 //
 // Bound by the products where tiles fill the chip (4096 x 8192 x 8192 in 128x256 tiles 506 us, 1.09 PFLOP/s), else by the slabs that
 // one workgroup takes in turn, 0.46 us each in 32x128 and 64x64 tiles: then workgroups share a tile's slabs, and their parts are added by a second
-// kernel (50 x 5000 x 4104 15.7 us alone, 11.9 by threes).
+// kernel (50 x 5000 x 4104 15.7 us alone, 11.7 by threes).  A slab's scales are a line of memory for each row: every one is requested once (by
+// each wave that had room: 512 x 1024 x 16384 36.8 us against 32.9).
 #pragma once
 
 #include "mx4_tile.h"
