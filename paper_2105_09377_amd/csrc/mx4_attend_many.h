@@ -45,7 +45,8 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
   uint32_t at = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
   const uint32_t part = at % uint32_t(a.parts);
   at /= uint32_t(a.parts);
-  const uint32_t row_tile = at % uint32_t(row_tiles), bh = at / uint32_t(row_tiles);
+  // (from the last row tile on: it sees the most, and short ones at the end leave less of the chip waiting)
+  const uint32_t bh = at / uint32_t(row_tiles), row_tile = uint32_t(row_tiles) - 1 - (at - bh * uint32_t(row_tiles));
   const uint32_t b = bh / uint32_t(a.cache.heads), head = bh - b * uint32_t(a.cache.heads);
   const int32_t row0 = int32_t(row_tile) * kRows, row1 = (row0 + kRows < rows ? row0 + kRows : rows) - 1;
   const int32_t len = length_of(a, b);
