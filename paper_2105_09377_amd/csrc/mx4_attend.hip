@@ -533,7 +533,11 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
 void plan(Mx4AttendArgs* a) {
   const int64_t rows = int64_t(a->queries) * a->group;
   const bool wide = a->cache.dim > 128;
-  a->tiles = rows > 128 && !wide ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
+  // 256 rows per workgroup, one of them on a compute unit; 128, two of them, where most tokens are queries themselves, so that row tiles differ in
+  // what they see, and there are few (2048 queries, 32 heads of 128 numbers on 8, 78.6 and 69.6 us; 2 x 4096 of them 324 and 339; 2 x 512 over
+  // 4096 tokens 91 and 102).
+  const bool uneven = a->width * a->cache.page <= 2 * int64_t(a->queries) && a->batch * a->cache.heads * ceil_div(rows, 256) <= 512;
+  a->tiles = rows > 128 && !wide && !uneven ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
   a->least = a->tiles >= 8 ? 4 : 8;
   a->slots = 0;
   const int64_t tasks = a->batch * a->cache.heads * ceil_div(rows, 16 * a->tiles), some = tasks > 0 ? tasks : 1;

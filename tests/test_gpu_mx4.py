@@ -432,7 +432,8 @@ def test_attend_without_pages():
 
 MANY_ROWS = [  # more than 32 rows of a cache head: tiles of 128 rows, the last of them partly empty
     (1, 33, 1, 1, 64, 16, 33), (2, 100, 2, 4, 64, 16, 400), (1, 129, 1, 1, 128, 32, 200), (2, 64, 1, 3, 96, 16, 1000), (1, 50, 2, 2, 192, 48, 700),
-    (1, 70, 1, 2, 256, 16, 600), (3, 130, 1, 1, 64, 64, 1500), (1, 40, 1, 1, 128, 16, 3000), (1, 9, 2, 16, 256, 64, 1300), (2, 257, 1, 1, 96, 128, 257)]
+    (1, 70, 1, 2, 256, 16, 600), (3, 130, 1, 1, 64, 64, 1500), (1, 40, 1, 1, 128, 16, 3000), (1, 9, 2, 16, 256, 64, 1300), (2, 257, 1, 1, 96, 128, 257),
+    (1, 150, 1, 2, 64, 16, 700), (2, 90, 1, 3, 128, 16, 400), (1, 300, 1, 1, 96, 32, 1000)]
 
 
 @pytest.mark.parametrize("batch,queries,heads,group,dim,page,longest", MANY_ROWS)
