@@ -1,7 +1,7 @@
 // Attention over a paged cache of microscaled 4-bit keys and values.
 //
 // A workgroup has 16 QT rows -- queries and heads that share the keys and values of one cache head -- and a part of
-// the sequence; its four waves take tiles of 64 tokens in turn, each with a running maximum and sum, and are
+// the sequence; its four waves (eight where there is a compute unit for every workgroup) take tiles of 64 tokens in turn, each with a running maximum and sum, and are
 // joined at the end; parts are joined by a second kernel.  Nothing passes through LDS on the way in: the cache's
 // order is the one that the matrix unit wants.  With r = lane % 16, g = lane / 16:
 //   scores: 16 tokens x 16 rows per product (16x16x32 bfloat16).  Lane (r, g) reads numbers g D/4 .. of the key of
@@ -23,8 +23,6 @@
 namespace gs {
 
 namespace {
-
-constexpr int kWaves = 4;
 
 // Maximum and sum over the four lanes that have the same r.
 __device__ __forceinline__ float max_over_g(float v) {
@@ -67,19 +65,19 @@ __device__ __forceinline__ void load_dwords(const uint8_t* p, uint32_t (&out)[N]
   }
 }
 
-template <int D, int QT>
+template <int D, int QT, int WV>
 struct AttendShape {
   static constexpr int C = D / 32;                       // blocks of 32; dwords of a lane's quarter of a key
   static constexpr int KS = (C == 2 || C == 4) ? 1 : 2;  // scale bytes that this quarter has
   static constexpr int VP = (D / 8 + 15) / 16;           // passes over the pieces of the values, 16 at a time
   static constexpr int kRow = D + 4;                     // floats of a row while waves are joined
   static constexpr int kRows = 16 * QT;
-  static constexpr size_t kLds = size_t(kWaves) * 16 * (kRow + 2) * 4;
+  static constexpr size_t kLds = size_t(WV) * 16 * (kRow + 2) * 4;
 };
 
-template <int D, int QT>
-__global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1) mx4_attend_kernel(Mx4AttendArgs a) {
-  using S = AttendShape<D, QT>;
+template <int D, int QT, int WV>
+__global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 2) : 1) mx4_attend_kernel(Mx4AttendArgs a) {
+  using S = AttendShape<D, QT, WV>;
   constexpr int C = S::C, KS = S::KS, VP = S::VP, kRows = S::kRows, kRow = S::kRow;
   extern __shared__ __attribute__((aligned(16))) float lds[];
 
@@ -368,11 +366,11 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1)
     Place at = place(i, ids);
     load_keys(at, keys);
     load_values(at, values);
-    find(i + kWaves, ids);
-    for (; i < stop; i += kWaves) {
-      const bool more = i + kWaves < stop;
-      const Place next = place(i + kWaves, ids);
-      find(i + 2 * kWaves, ids);
+    find(i + WV, ids);
+    for (; i < stop; i += WV) {
+      const bool more = i + WV < stop;
+      const Place next = place(i + WV, ids);
+      find(i + 2 * WV, ids);
       compute(at, next, more, keys, values);
       if (more) load_values(next, values);
       at = next;
@@ -381,7 +379,7 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1)
 
   // join the waves, 16 rows at a time
   float* const my_o = lds + wave * 16 * kRow;
-  float* const ml = lds + kWaves * 16 * kRow;            // [wave][row][2]
+  float* const ml = lds + WV * 16 * kRow;            // [wave][row][2]
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
     const float sum = sum_over_g(l[u][0]);
@@ -401,14 +399,14 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1)
             *reinterpret_cast<f32x4*>(my_o + r * kRow + piece * 8 + j) = f32x4{o[u][p][j][i], o[u][p][j + 1][i], o[u][p][j + 2][i], o[u][p][j + 3][i]};
       }
     __syncthreads();
-    const int rr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    const int rr = threadIdx.x >> 4 & 15, d0 = (threadIdx.x & 15) * (D / 16);
     float top = -__builtin_inff();
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * 16 + rr) * 2]);
+    for (int v = 0; v < WV; ++v) top = fmaxf(top, ml[(v * 16 + rr) * 2]);
     const float ref = top == -__builtin_inff() ? 0.0f : top;
-    float total = 0, f[kWaves];
+    float total = 0, f[WV];
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
+    for (int v = 0; v < WV; ++v) {
       f[v] = exp2_fast(ml[(v * 16 + rr) * 2] - ref);
       total += f[v] * ml[(v * 16 + rr) * 2 + 1];
     }
@@ -417,10 +415,10 @@ __global__ void __launch_bounds__(kWaves * 64, QT == 1 ? (D <= 128 ? 3 : 2) : 1)
     for (int d = 0; d < D / 16; ++d) {
       x[d] = 0;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) x[d] += f[v] * lds[(v * 16 + rr) * kRow + d0 + d];
+      for (int v = 0; v < WV; ++v) x[d] += f[v] * lds[(v * 16 + rr) * kRow + d0 + d];
     }
     const int32_t row = row0 + u * 16 + rr;
-    if (row >= rows) continue;
+    if (threadIdx.x >= 256 || row >= rows) continue;     // (16 lanes to a row)
     if (cut.parts == 1) {
       const float inv = total != 0.0f ? 1.0f / total : 0.0f;
       const int32_t i = row / a.group, h = row - i * a.group;
@@ -552,6 +550,10 @@ void plan(Mx4AttendArgs* a) {
   int64_t parts = a->tiles >= 8 ? (groups + some / 2) / some : ceil_div(groups, some);
   parts = parts < useful ? parts : useful;
   parts = parts < kMaxParts ? parts : kMaxParts;
+  // A second launch takes as long as two tiles of a wave that has a unit for itself, and as four where others share it: 8 sequences of 700 tokens (8
+  // cache heads of 128 numbers) 8.7 us in one part, 11.4 in two, one of 1500 13.0 and 11.4; 64 of 1000 15.7 and 20.8.
+  const int64_t few = tasks > 256 ? 16 : a->tiles == 1 && !wide ? 16 : 8;
+  if (a->tiles <= 2 && ceil_div(most, kTile) <= few) parts = 1;
   a->parts = int32_t(parts > 1 ? parts : 1);
   // Lengths that differ are no reason to wait for the longest, where the sequences are few enough for a workgroup to look at all.
   if (a->parts > 1 && a->tiles <= 2 && a->batch <= 64 && groups / a->cache.heads > a->batch) {
@@ -564,7 +566,7 @@ int64_t results_of(const Mx4AttendArgs& a) {     // workgroups
   return a.batch * a.cache.heads * ceil_div(int64_t(a.queries) * a.group, 16 * a.tiles) * a.parts;
 }
 
-template <int D, int QT>
+template <int D, int QT, int WV>
 hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   constexpr bool kMany = QT >= 8;
   constexpr int kRows = 16 * QT;
@@ -575,15 +577,15 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   void (*kernel)(Mx4AttendArgs);
   size_t lds;
   if constexpr (kMany) {
-    kernel = mx4_attend_many_kernel<D, QT / 2>;
-    lds = ManyShape<D, QT / 2>::kLds;
+    kernel = mx4_attend_many_kernel<D, WV>;
+    lds = ManyShape<D, WV>::kLds;
   } else {
-    kernel = mx4_attend_kernel<D, QT>;
-    lds = AttendShape<D, QT>::kLds;
+    kernel = mx4_attend_kernel<D, QT, WV>;
+    lds = AttendShape<D, QT, WV>::kLds;
   }
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kMany ? QT * 32 : kWaves * 64), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(WV * 64), lds, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
@@ -596,8 +598,11 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
 template <int D>
 hipError_t launch_d(const Mx4AttendArgs& a, hipStream_t s) {
   if constexpr (D <= 128)
-    if (a.tiles == 16) return launch<D, 16>(a, s);
-  return a.tiles == 1 ? launch<D, 1>(a, s) : a.tiles == 2 ? launch<D, 2>(a, s) : launch<D, 8>(a, s);
+    if (a.tiles == 16) return launch<D, 16, 8>(a, s);
+  if (a.tiles == 8) return launch<D, 8, 4>(a, s);
+  if (a.tiles == 2) return launch<D, 2, 4>(a, s);
+  // 32 sequences of 500 tokens, 8 cache heads: 8.4 us with four waves, 7.9 with eight
+  return results_of(a) > 256 ? launch<D, 1, 4>(a, s) : launch<D, 1, 8>(a, s);
 }
 
 }  // namespace
