@@ -146,6 +146,13 @@ struct Mx4AttendArgs {
   FastDiv by_group, by_rows, by_heads, by_parts;      // rows: queries * group
   int32_t slots;          // parts of all sequences together where they are cut to the same length, else 0
 };
+// How an attention is done.
+struct Mx4AttendPlan {
+  int rows, waves;        // of a workgroup
+  int parts, slots;       // of a sequence at most; of all sequences together where they are cut to the same length, else 0
+  bool joined_alone;      // a row's parts have a workgroup to join them
+};
+Mx4AttendPlan mx4_attend_plan(const Mx4AttendArgs& a);
 hipError_t launch_mx4_attend(const Mx4AttendArgs& a, hipStream_t s);
 size_t mx4_attend_workspace(const Mx4AttendArgs& a);
 

@@ -322,4 +322,25 @@ size_t glenside_mx4_attend_workspace(const gs_ap* q, const gs_mx4_cache* cache, 
   return mx4_attend_workspace(a);
 }
 
+// For tests, not part of the interface: how a product (Mx4DotWay, workgroups that share a sum) and an attention (Mx4AttendPlan) of
+// these sizes are done.  Host only.
+int gs_test_mx4_dot_plan(int x_is_bf16, int64_t M, int64_t N, int64_t K, int plan[2]) {
+  const Mx4DotPlan p = plan_mx4_dot(x_is_bf16 != 0, M, N, K);
+  plan[0] = p.way;
+  plan[1] = p.splits;
+  return GS_OK;
+}
+int gs_test_mx4_attend_plan(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table, int64_t window, int64_t sinks, int plan[5]) {
+  Mx4AttendArgs a;
+  const int st = attend_args(q, cache, table, window, sinks, false, &a);
+  if (st) return st;
+  const Mx4AttendPlan p = mx4_attend_plan(a);
+  plan[0] = p.rows;
+  plan[1] = p.waves;
+  plan[2] = p.parts;
+  plan[3] = p.slots;
+  plan[4] = p.joined_alone;
+  return GS_OK;
+}
+
 }  // extern "C"

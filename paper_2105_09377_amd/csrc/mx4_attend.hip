@@ -565,6 +565,13 @@ int64_t results_of(const Mx4AttendArgs& a) {     // workgroups
   if (a.slots) return int64_t(a.slots) * a.cache.heads;
   return a.batch * a.cache.heads * ceil_div(int64_t(a.queries) * a.group, 16 * a.tiles) * a.parts;
 }
+// Waves of a workgroup.  32 sequences of 500 tokens, 8 cache heads: 8.4 us with four, 7.9 with eight.
+int waves_of(const Mx4AttendArgs& a) {
+  if (a.tiles == 16) return 8;
+  return a.tiles == 1 && results_of(a) <= 256 ? 8 : 4;
+}
+// Whether the parts of a row have a workgroup to join them.
+bool joined_alone(const Mx4AttendArgs& a) { return a.slots ? a.slots / a.batch >= 8 : a.parts > 8; }
 
 template <int D, int QT, int WV>
 hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
@@ -589,7 +596,7 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
-    if (a.slots ? a.slots / a.batch >= 8 : a.parts > 8) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
+    if (joined_alone(a)) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
     else hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, false>), dim3(unsigned(ceil_div(total_rows, kJoined))), dim3(256), 0, s, a, int32_t(total_rows));
     e = hipGetLastError();
   }
@@ -601,11 +608,16 @@ hipError_t launch_d(const Mx4AttendArgs& a, hipStream_t s) {
     if (a.tiles == 16) return launch<D, 16, 8>(a, s);
   if (a.tiles == 8) return launch<D, 8, 4>(a, s);
   if (a.tiles == 2) return launch<D, 2, 4>(a, s);
-  // 32 sequences of 500 tokens, 8 cache heads: 8.4 us with four waves, 7.9 with eight
-  return results_of(a) > 256 ? launch<D, 1, 4>(a, s) : launch<D, 1, 8>(a, s);
+  return waves_of(a) == 4 ? launch<D, 1, 4>(a, s) : launch<D, 1, 8>(a, s);
 }
 
 }  // namespace
+
+Mx4AttendPlan mx4_attend_plan(const Mx4AttendArgs& given) {
+  Mx4AttendArgs a = given;
+  plan(&a);
+  return Mx4AttendPlan{16 * a.tiles, waves_of(a), a.parts, a.slots, a.parts > 1 && joined_alone(a)};
+}
 
 size_t mx4_attend_workspace(const Mx4AttendArgs& given) {
   Mx4AttendArgs a = given;
