@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
     for (int c = 0; c < C; ++c) q[t][c] = ok ? scaled_signs(*reinterpret_cast<const i32x4*>(src + 8 * c), a.scale) : i32x4{0, 0, 0, 0};
   }
   const int32_t pos_first = len - a.queries + row0 / a.group, pos_last = len - a.queries + row1 / a.group;
-  const float to_log2 = positive_scale(a.scale);
+  const ScoreScale unit(a.scale);
 
   f32x4 o[QT][VP][8], l[QT];
   float m[QT];
@@ -229,6 +229,7 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
     const bool all_seen = at.pages == 15u && at.token + kTile - 1 <= pos_first && (pos_last - at.token < window || at.token + kTile <= sinks);
     // weights, as the products with the values want them: p[row tile][half of the tile]
     i32x4 w[QT][2];
+    float ref[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       if (!all_seen) {
@@ -245,10 +246,10 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
       float top = s[u][0][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[u][i / 4][i % 4]);
-      top = fmaxf(max_over_g(top) * to_log2 + kHeadroom, m[u]);
-      const float ref = top == -__builtin_inff() ? 0.0f : top;
+      top = fmaxf(unit.score(max_over_g(top)) + kHeadroom, m[u]);
+      ref[u] = top == -__builtin_inff() ? 0.0f : top;
       if (__any(top > m[u])) {
-        const float shrink = exp2_fast(m[u] - ref);
+        const float shrink = exp2_fast(m[u] - ref[u]);
         m[u] = top;
         l[u] *= shrink;
 #pragma unroll
@@ -256,12 +257,28 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
 #pragma unroll
           for (int j = 0; j < 8; ++j) o[u][p][j] *= shrink;
       }
+    }
+    bool far = false;                                  // (in one branch for all rows: one each 2 % more for 32 rows)
+#pragma unroll
+    for (int u = 0; u < QT; ++u) far = far || ScoreScale::far(ref[u]);
+    if (__builtin_expect(__any(far), 0)) {
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[u][n][i] = unit.apart(s[u][n][i], ref[u]);
+        ref[u] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const f32x4 x = s[u][2 * h + i / 2];
-          w[u][h][i] = int32_t(pack_bf16x2(exp2_fast(fmaf(x[2 * i % 4], to_log2, -ref)), exp2_fast(fmaf(x[2 * i % 4 + 1], to_log2, -ref))));
+          w[u][h][i] = int32_t(pack_bf16x2(exp2_fast(fmaf(x[2 * i % 4], unit.to_log2, -ref[u])), exp2_fast(fmaf(x[2 * i % 4 + 1], unit.to_log2, -ref[u]))));
         }
 #pragma unroll
       for (int n = 0; n < 4; ++n) l[u] = add_weights(w[u][n / 2][2 * n % 4], w[u][n / 2][2 * n % 4 + 1], l[u]);

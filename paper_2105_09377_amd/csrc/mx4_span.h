@@ -111,9 +111,24 @@ __device__ __forceinline__ i32x4 scaled_signs(i32x4 q, float scale) {
   }
   return q;
 }
-__device__ __forceinline__ float positive_scale(float scale) {
-  return scale == 0 ? 1.0f : fmaxf(fabsf(scale) * 1.44269504088896340736f, 1.17549435e-38f);
-}
+// Products times the scale and log2(e) are scores in the unit of the weights, 2^(score - m), m being the largest one and the headroom.  One
+// fused multiplication and subtraction gives that power; it does not round the score, as m is rounded, so all weights of a row are off by the
+// same power, up to half a unit in the last place of the scores: 2 where they are 2^25, beyond the numbers' range where they are above 2^31.  So
+// where a row of the wave has a score that is `far`, scores are rounded first and products replaced by what they are `apart` from m: the largest
+// one's weight is that of the headroom, or 1 where the headroom is less than such a unit.
+struct ScoreScale {
+  float to_log2;                     // above 0
+  __device__ explicit ScoreScale(float given) : to_log2(given == 0 ? 1.0f : fmaxf(fabsf(given) * 1.44269504088896340736f, 1.17549435e-38f)) {}
+  __device__ float score(float product) const {
+#pragma clang fp contract(off)
+    return product * to_log2;
+  }
+  __device__ float apart(float product, float ref) const {
+#pragma clang fp contract(off)
+    return (score(product) - ref) / to_log2;
+  }
+  static __device__ bool far(float m) { return fabsf(m) > 268435456.0f; }      // 2^28
+};
 
 // The sum of a lane's four weights (two dwords of bfloat16), added to each of the four numbers of l: a product of 4x4x4 with ones.  The
 // rounded weights are summed, those that the values are multiplied with.
