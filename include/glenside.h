@@ -375,9 +375,10 @@ int glenside_mx4_cache_read(const gs_mx4_cache* cache, const gs_ap* table, const
  * (window 0: all t <= p), except tokens in entries that are no page.
  *   out[b,i,h] = sum_t softmax_t(scale q[b,i,h] . k[b,t,h / G]) v[b,t,h / G],   G = query heads / cache heads.
  * A query that sees nothing, or whose scores are all -infinity, gives zeros; tokens that a query does not see
- * have no part in its result, whatever they hold.  Scores, weights and sums are fp32, weights are rounded to bf16
- * for their product with the values and for their sum.  q ((batch, Lq, G heads),(head_dim)) bf16; out of its shape and split, bf16 or f32;
- * lengths i32 ((batch),()), taken as at least 0 and at most W P.
+ * have no part in its result, whatever they hold.  Scores, weights and sums are fp32 (scores beyond 2.358e38, which
+ * times log2(e) are infinite, count as that), weights are rounded to bf16 for their product with the values and for
+ * their sum.  scale: below 2.358e38 in magnitude, for the same reason.  q ((batch, Lq, G heads),(head_dim)) bf16; out
+ * of its shape and split, bf16 or f32; lengths i32 ((batch),()), taken as at least 0 and at most W P.
  * workspace: glenside_mx4_attend_workspace bytes (may be 0; 16-byte aligned).                       */
 int glenside_mx4_attend(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table, const gs_ap* lengths,
                         float scale, int64_t window, int64_t sinks, gs_ap* out, void* workspace,

@@ -305,7 +305,7 @@ int glenside_mx4_attend(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* 
   if (out->rank != q->rank || out->n_access != q->n_access) return GS_ERR_RANK;
   if (!same_pattern_shape(out, q)) return GS_ERR_SHAPE;
   if (out->dtype != GS_BF16 && out->dtype != GS_F32) return GS_ERR_DTYPE;
-  if (!isfinite(scale)) return GS_ERR_UNSUPPORTED;
+  if (!isfinite(scale * 1.44269504088896340736f)) return GS_ERR_UNSUPPORTED;     // (the unit that scores are computed in)
   a.lengths = static_cast<const int32_t*>(lengths->data);
   a.out = out->data;
   a.out_dtype = out->dtype;

@@ -75,3 +75,17 @@ def test_attention_with_far_scores_of_both_signs(queries, group, dim):
     q[0, far] = 0.0
     q[0, far, 0] = -2.0 ** 33                    # the mean over a third of the tokens
     check_attention(q.to(BF), cache, table, tokens, 1.0)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127, -2.0 ** 127, 2.358e38])
+@pytest.mark.parametrize("queries,group,dim", KERNELS)
+def test_attention_with_the_largest_scales(queries, group, dim, scale):
+    """Up to those that are refused: scores of zero, scores of some units, and scores so far apart that one token has all weight."""
+    tokens = 70
+    k, v = normal((tokens, 1, dim), 11, F32), normal((tokens, 1, dim), 12, F32)
+    cache, table = cached(k, v, 16)
+    q = normal((1, queries, group, dim), 13, F32)
+    tiny = q * 2.0 ** -128                       # numbers below bfloat16's normal ones, scores of some units
+    tiny[:, :, 0] = 0.0                          # the mean of the values
+    check_attention(tiny.to(BF), cache, table, tokens, scale)
+    check_attention((q * 2.0 ** -60).to(BF), cache, table, tokens, scale)

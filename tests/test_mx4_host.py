@@ -221,3 +221,12 @@ def test_binding_refuses_caches():
         gs.mx4_attend(k.transpose(1, 2), c, table, n, 1.0)
     with pytest.raises(TypeError):
         gs.mx4_attend(k, c, table, n, "1")
+
+
+@pytest.mark.parametrize("scale", [2.36e38, -2.36e38, 3.0e38, 3.4028234e38])
+def test_attention_refuses_scales_whose_unit_is_infinite(scale):
+    """Scores are computed times log2 e; up to that line a call gets as far as the check of its workspace."""
+    for given, status in ((scale, gs.GS_ERR_UNSUPPORTED), (scale / abs(scale) * 2.358e38, gs.GS_ERR_WORKSPACE)):
+        a = attention(table=ap((3, 500), 1, I32), scale=given)
+        assert gs.lib().glenside_mx4_attend(ref(a["q"]), ref(a["cache"]), ref(a["table"]), ref(a["lengths"]), a["scale"], a["window"], a["sinks"],
+                                            ref(a["out"]), a["ws"], a["bytes"], None) == status
