@@ -118,7 +118,7 @@ __device__ __forceinline__ i32x4 scaled_signs(i32x4 q, float scale) {
 // one's weight is that of the headroom, or 1 where the headroom is less than such a unit.
 struct ScoreScale {
   float to_log2;                     // above 0
-  __device__ explicit ScoreScale(float given) : to_log2(given == 0 ? 1.0f : fmaxf(fabsf(given) * 1.44269504088896340736f, 1.17549435e-38f)) {}
+  __device__ explicit ScoreScale(float given) : to_log2(given == 0 ? 1.0f : fabsf(given) * 1.44269504088896340736f) {}
   __device__ float score(float product) const {
 #pragma clang fp contract(off)
     return product * to_log2;

@@ -89,3 +89,15 @@ def test_attention_with_the_largest_scales(queries, group, dim, scale):
     tiny[:, :, 0] = 0.0                          # the mean of the values
     check_attention(tiny.to(BF), cache, table, tokens, scale)
     check_attention((q * 2.0 ** -60).to(BF), cache, table, tokens, scale)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -125, 1e-39, -1e-39, 2.0 ** -134])
+@pytest.mark.parametrize("queries,group,dim", KERNELS)
+def test_attention_with_the_smallest_scales(queries, group, dim, scale):
+    """Scales beyond float's normal numbers, and queries so large that scores are some units all the same (2^-134 has 16 bits left: off by 2^-17 of scores
+    below 8)."""
+    tokens = 60
+    k, v = normal((tokens, 1, dim), 41, F32), normal((tokens, 1, dim), 42, F32)
+    cache, table = cached(0.25 * k, v, 16)
+    q = normal((1, queries, group, dim), 43, F32) * 2.0 ** 122
+    check_attention(q.to(BF), cache, table, tokens, scale)
