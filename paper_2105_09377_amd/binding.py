@@ -509,11 +509,12 @@ def mx4_weight_dot(x: torch.Tensor, w: Mx4, n_access: Optional[int] = None, out_
 def mx4_cache(n_pages: int, heads: int, page_size: int, head_dim: int, device) -> Mx4Cache:
     """A new cache, every number zero."""
     d = gs_mx4_cache()
-    d.n_pages, d.heads, d.page_size, d.head_dim = n_pages, heads, page_size, head_dim
+    some = n_pages or 1                          # (a cache without pages is one; its blocks have a size too)
+    d.n_pages, d.heads, d.page_size, d.head_dim = some, heads, page_size, head_dim
     need = int(lib().glenside_mx4_cache_bytes(ctypes.byref(d)))
     if need == 0:
         raise GlensideError(GS_ERR_UNSUPPORTED, "mx4_cache")
-    return Mx4Cache(torch.zeros((n_pages, heads, need // (n_pages * heads)), dtype=torch.uint8, device=device), page_size, head_dim)
+    return Mx4Cache(torch.zeros((n_pages, heads, need // (some * heads)), dtype=torch.uint8, device=device), page_size, head_dim)
 
 
 def mx4_cache_append(cache: Mx4Cache, table: torch.Tensor, first: torch.Tensor, k: torch.Tensor, v: torch.Tensor,

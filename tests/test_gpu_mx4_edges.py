@@ -101,3 +101,16 @@ def test_attention_with_the_smallest_scales(queries, group, dim, scale):
     cache, table = cached(0.25 * k, v, 16)
     q = normal((1, queries, group, dim), 43, F32) * 2.0 ** 122
     check_attention(q.to(BF), cache, table, tokens, scale)
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_a_cache_without_pages(queries):
+    """Tokens are dropped, read back as zeros, and seen by nobody."""
+    cache = gs.mx4_cache(0, 2, 16, 64, DEV)
+    table = torch.zeros(3, 5, dtype=torch.int32, device=DEV)
+    n = torch.tensor([80, 0, 7], dtype=torch.int32, device=DEV)
+    k = normal((3, 9, 2, 64), 51).to(DEV)
+    gs.mx4_cache_append(cache, table, n, k, k)
+    for got in gs.mx4_cache_read(cache, table, n, 9):
+        assert got.shape == k.shape and not got.any()
+    assert not gs.mx4_attend(normal((3, queries, 4, 64), 52).to(DEV), cache, table, n, 0.1).any()

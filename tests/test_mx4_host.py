@@ -230,3 +230,10 @@ def test_attention_refuses_scales_whose_unit_is_infinite(scale):
         a = attention(table=ap((3, 500), 1, I32), scale=given)
         assert gs.lib().glenside_mx4_attend(ref(a["q"]), ref(a["cache"]), ref(a["table"]), ref(a["lengths"]), a["scale"], a["window"], a["sinks"],
                                             ref(a["out"]), a["ws"], a["bytes"], None) == status
+
+
+def test_a_cache_without_pages():
+    c = gs.mx4_cache(0, 2, 32, 64, "cpu")
+    assert c.data.shape == (0, 2, 32 * 64 + 2 * 32 * 2) and (c.page_size, c.head_dim) == (32, 64)
+    refused(gs.GS_ERR_UNSUPPORTED, gs.mx4_cache, 0, 2, 30, 64, "cpu")
+    refused(gs.GS_ERR_UNSUPPORTED, gs.mx4_cache, -1, 2, 32, 64, "cpu")
