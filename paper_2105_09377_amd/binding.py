@@ -508,6 +508,8 @@ def mx4_weight_dot(x: torch.Tensor, w: Mx4, n_access: Optional[int] = None, out_
 
 def mx4_cache(n_pages: int, heads: int, page_size: int, head_dim: int, device) -> Mx4Cache:
     """A new cache, every number zero."""
+    if max(n_pages, heads, page_size, head_dim) > 0x7fffffff or min(n_pages, heads, page_size, head_dim) < 0:
+        raise GlensideError(GS_ERR_UNSUPPORTED, "mx4_cache")      # (the descriptor's fields would keep the low bits)
     d = gs_mx4_cache()
     some = n_pages or 1                          # (a cache without pages is one; its blocks have a size too)
     d.n_pages, d.heads, d.page_size, d.head_dim = some, heads, page_size, head_dim

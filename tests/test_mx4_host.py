@@ -237,3 +237,10 @@ def test_a_cache_without_pages():
     assert c.data.shape == (0, 2, 32 * 64 + 2 * 32 * 2) and (c.page_size, c.head_dim) == (32, 64)
     refused(gs.GS_ERR_UNSUPPORTED, gs.mx4_cache, 0, 2, 30, 64, "cpu")
     refused(gs.GS_ERR_UNSUPPORTED, gs.mx4_cache, -1, 2, 32, 64, "cpu")
+
+
+@pytest.mark.parametrize("sizes", [(4, (1 << 32) + 2, 32, 64), (4, 2, (1 << 32) + 32, 64), (4, 2, 32, (1 << 32) + 64), ((1 << 64) + 4, 2, 32, 64),
+                                   (4, 2 - (1 << 32), 32, 64)])
+def test_a_cache_of_sizes_beyond_the_descriptor(sizes):
+    """32 bits of such a size are a possible one."""
+    refused(gs.GS_ERR_UNSUPPORTED, gs.mx4_cache, *sizes, "cpu")
