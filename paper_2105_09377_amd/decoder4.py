@@ -49,7 +49,7 @@ class Decoder4Stack:
             v = gs.mx4_weight_dot(rows, w["v"], out_dtype=bf16).view(batch, tokens, self.kv_heads, self.head_dim)
             gs.mx4_cache_append(cache, table, first, k, v)
             a = gs.mx4_attend(q, cache, table, lengths, scale=self.head_dim ** -0.5, window=self.window, sinks=self.sinks)
-            a = gs.mx4_weight_dot(a.view(rows.shape[0], -1), w["o"], out_dtype=bf16)
+            a = gs.mx4_weight_dot(a.view(rows.shape[0], self.heads * self.head_dim), w["o"], out_dtype=bf16)
             rows = gs.pair_reduce(rows, a)
             if small:
                 h = gs.mx4_dot(gs.mx4_quantize(rows), w["up"], out_dtype=bf16, act=gs.GS_ACT_RELU)
