@@ -9,7 +9,6 @@ constexpr int kMx4Block = 32;        // numbers that share a scale; 16 bytes
 constexpr int kMx4ScaleRun = 8;      // rows of scale bytes are padded to multiples of this
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 
 __host__ __device__ inline int64_t mx4_blocks(int64_t k) { return ceil_div(k, kMx4Block); }
 __host__ __device__ inline int64_t mx4_scale_pitch(int64_t k) { return round_up(mx4_blocks(k), kMx4ScaleRun); }

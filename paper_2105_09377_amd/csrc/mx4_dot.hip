@@ -23,49 +23,42 @@ __device__ __forceinline__ f32x4 mfma_mx4(const i32x4& a, const i32x4& b, const 
 typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---------------------------------------------------------------------------------------------
-// Few rows of x: NW waves share a tile of 16 MT rows of x and 16 NT rows of w, the units of K dealt to them, their
+// Few rows of x: eight waves share a tile of 16 rows of x and 16 NT rows of w, the units of K dealt to them, their
 // partial tiles added at the end in the order of the waves.  Everything goes from memory to registers, the next unit's
 // loads in flight while one is multiplied: w is read once, and bound by that: one row with 8192 x 8192 weights 10.2 us, 3.5 TB/s from
 // a standing start (11.9 with weights that are in no cache; four units in flight 12.8, and lanes without a row of x switched off 11.8).
 // ---------------------------------------------------------------------------------------------
-template <bool XBF, int MT, int NT, int NW>
-__global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uint32_t tiles_n) {
-  __shared__ f32x4 part[NW][MT * NT][64];
+constexpr int kRowWaves = 8;
+template <bool XBF, int NT>
+__global__ void __launch_bounds__(kRowWaves * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uint32_t tiles_n) {
+  constexpr int NW = kRowWaves;
+  __shared__ f32x4 part[NW][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int64_t m0 = int64_t(tm) * 16 * MT, n0 = int64_t(tn) * 16 * NT;
+  const int64_t m0 = int64_t(tm) * 16, n0 = int64_t(tn) * 16 * NT;
   const int64_t nb = mx4_blocks(a.K), pitch = mx4_scale_pitch(a.K);
   const int32_t units = int32_t(pitch / 8);
 
   // a lane's rows; those behind the end are the last one, and their results are not stored
-  const uint8_t *wp[NT], *wsp[NT], *xp[MT], *xsp[MT];
+  const uint8_t *wp[NT], *wsp[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int64_t row = n0 + n * 16 + r < a.N ? n0 + n * 16 + r : a.N - 1;
     wp[n] = static_cast<const uint8_t*>(a.w) + row * nb * 16 + g * 32;
     wsp[n] = a.ws + row * pitch + g * 2;
   }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int64_t row = m0 + m * 16 + r < a.M ? m0 + m * 16 + r : a.M - 1;
-    if constexpr (XBF) {
-      xp[m] = static_cast<const uint8_t*>(a.x) + (row * a.K + g * 64) * 2;
-    } else {
-      xp[m] = static_cast<const uint8_t*>(a.x) + row * nb * 16 + g * 32;
-      xsp[m] = a.xs + row * pitch + g * 2;
-    }
-  }
+  const int64_t x_row = m0 + r < a.M ? m0 + r : a.M - 1;
+  const uint8_t* const xp = static_cast<const uint8_t*>(a.x) + (XBF ? (x_row * a.K + g * 64) * 2 : x_row * nb * 16 + g * 32);
+  const uint8_t* const xsp = XBF ? nullptr : a.xs + x_row * pitch + g * 2;
 
-  f32x4 acc[MT][NT];
+  f32x4 acc[NT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0, 0, 0, 0};
+  for (int n = 0; n < NT; ++n) acc[n] = f32x4{0, 0, 0, 0};
 
   constexpr int XP = XBF ? 8 : 2;          // 16-byte pieces of a lane's two blocks of x
   struct Unit {
-    i32x4 w[NT][2], x[MT][XP];
-    uint32_t ws[NT], xs[MT];
+    i32x4 w[NT][2], x[XP];
+    uint32_t ws[NT], xs;
   };
   auto load = [&](int32_t u, Unit& t) {
     // blocks behind K are read as zeros
@@ -82,49 +75,38 @@ __global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uin
       }
     }
     if constexpr (!XBF) {
+      t.xs = *reinterpret_cast<const uint16_t*>(xsp + at);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        t.xs[m] = *reinterpret_cast<const uint16_t*>(xsp[m] + at);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          t.x[m][s] = i32x4{0, 0, 0, 0};
-          if (whole || s < left) t.x[m][s] = *reinterpret_cast<const i32x4*>(xp[m] + at * 16 + s * 16);
-        }
+      for (int s = 0; s < 2; ++s) {
+        t.x[s] = i32x4{0, 0, 0, 0};
+        if (whole || s < left) t.x[s] = *reinterpret_cast<const i32x4*>(xp + at * 16 + s * 16);
       }
+    } else if (at * 32 + 256 <= a.K) {                    // (uniform)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) t.x[c] = *reinterpret_cast<const i32x4_any2t*>(xp + at * 64 + c * 16);
     } else {
       const int64_t numbers = a.K - at * 32 - g * 64;     // of the lane's part of this row
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        if (m == 0 || m0 + m * 16 < a.M) {                // (uniform)
-          if (at * 32 + 256 <= a.K) {                     // (uniform)
+      for (int c = 0; c < 8; ++c) {
+        t.x[c] = i32x4{0, 0, 0, 0};
+        const uint16_t* src = reinterpret_cast<const uint16_t*>(xp + at * 64) + c * 8;
+        if (c * 8 + 8 <= numbers) {
+          t.x[c] = *reinterpret_cast<const i32x4_any2t*>(src);
+        } else {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) t.x[m][c] = *reinterpret_cast<const i32x4_any2t*>(xp[m] + at * 64 + c * 16);
-          } else {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              t.x[m][c] = i32x4{0, 0, 0, 0};
-              const uint16_t* src = reinterpret_cast<const uint16_t*>(xp[m] + at * 64) + c * 8;
-              if (c * 8 + 8 <= numbers) {
-                t.x[m][c] = *reinterpret_cast<const i32x4_any2t*>(src);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                  if (c * 8 + e < numbers) t.x[m][c][e / 2] |= int32_t(uint32_t(src[e]) << (16 * (e & 1)));
-              }
-            }
-          }
+          for (int e = 0; e < 7; ++e)
+            if (c * 8 + e < numbers) t.x[c][e / 2] |= int32_t(uint32_t(src[e]) << (16 * (e & 1)));
         }
+      }
     }
   };
   auto multiply = [&](const Unit& t) {
     if constexpr (!XBF) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          acc[m][n] = mfma_mx4(t.w[n][0], t.x[m][0], acc[m][n], int(t.ws[n]), int(t.xs[m]), std::integral_constant<int, 0>{});
-          acc[m][n] = mfma_mx4(t.w[n][1], t.x[m][1], acc[m][n], int(t.ws[n]), int(t.xs[m]), std::integral_constant<int, 1>{});
-        }
+      for (int n = 0; n < NT; ++n) {
+        acc[n] = mfma_mx4(t.w[n][0], t.x[0], acc[n], int(t.ws[n]), int(t.xs), std::integral_constant<int, 0>{});
+        acc[n] = mfma_mx4(t.w[n][1], t.x[1], acc[n], int(t.ws[n]), int(t.xs), std::integral_constant<int, 1>{});
+      }
     } else {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -136,10 +118,7 @@ __global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uin
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             const bf16x8 wv = __builtin_bit_cast(bf16x8, mx4_decode8(uint32_t(t.w[n][s][c]), sc[n]));
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-              if (m == 0 || m0 + m * 16 < a.M)
-                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, t.x[m][4 * s + c]), acc[m][n], 0, 0, 0);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, t.x[4 * s + c]), acc[n], 0, 0, 0);
           }
       }
     }
@@ -156,28 +135,26 @@ __global__ void __launch_bounds__(NW * 64) mx4_dot_rows_kernel(Mx4DotArgs a, uin
     multiply(cur);
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < NT; ++n) part[wave][m * NT + n][lane] = acc[m][n];
+  for (int n = 0; n < NT; ++n) part[wave][n][lane] = acc[n];
   __syncthreads();
-  for (int t = wave; t < MT * NT; t += NW) {
+  for (int t = wave; t < NT; t += NW) {
     f32x4 sum = part[0][t][lane];
 #pragma unroll
     for (int w = 1; w < NW; ++w) sum += part[w][t][lane];
-    const int64_t m = m0 + (t / NT) * 16 + r;
+    const int64_t m = m0 + r;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int64_t n = n0 + (t % NT) * 16 + 4 * g + e;
+      const int64_t n = n0 + t * 16 + 4 * g + e;
       if (m < a.M && n < a.N) store_result<float>(a.out, nullptr, a.out_dtype, m * a.N + n, sum[e], a.relu);
     }
   }
 }
 
-template <bool XBF, int MT, int NT, int NW>
+template <bool XBF, int NT>
 hipError_t launch_rows(const Mx4DotArgs& a, hipStream_t s) {
-  const int64_t tiles_m = ceil_div(a.M, 16 * MT), tiles_n = ceil_div(a.N, 16 * NT);
+  const int64_t tiles_m = ceil_div(a.M, 16), tiles_n = ceil_div(a.N, 16 * NT);
   if (tiles_m * tiles_n > 0x7fffffff || a.K >= (int64_t(1) << 38)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((mx4_dot_rows_kernel<XBF, MT, NT, NW>), dim3(unsigned(tiles_m * tiles_n)), dim3(NW * 64), 0, s, a, uint32_t(tiles_n));
+  hipLaunchKernelGGL((mx4_dot_rows_kernel<XBF, NT>), dim3(unsigned(tiles_m * tiles_n)), dim3(kRowWaves * 64), 0, s, a, uint32_t(tiles_n));
   return hipGetLastError();
 }
 
@@ -323,8 +300,8 @@ hipError_t launch_mx4_dot(const Mx4DotArgs& given, const Mx4DotPlan& p, void* wo
   }
   hipError_t e = hipErrorInvalidValue;
   switch (p.way) {
-    case kRows1: e = a.xs ? launch_rows<false, 1, 1, 8>(a, s) : launch_rows<true, 1, 1, 8>(a, s); break;
-    case kRows2: e = a.xs ? launch_rows<false, 1, 2, 8>(a, s) : launch_rows<true, 1, 2, 8>(a, s); break;
+    case kRows1: e = a.xs ? launch_rows<false, 1>(a, s) : launch_rows<true, 1>(a, s); break;
+    case kRows2: e = a.xs ? launch_rows<false, 2>(a, s) : launch_rows<true, 2>(a, s); break;
     case kTile64x64Few: e = launch_mx4_tiles<64, 64, 2, 2, 4>(a, s); break;
     case kTile64x64: e = launch_mx4_tiles<64, 64, 2, 2, 2>(a, s); break;
     case kTile128x128Few: e = launch_mx4_tiles<128, 128, 2, 4, 4>(a, s); break;
