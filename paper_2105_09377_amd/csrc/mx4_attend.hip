@@ -1,9 +1,10 @@
 // Attention over a paged cache of microscaled 4-bit keys and values.
 //
 // A workgroup has 16 QT rows -- queries and heads that share the keys and values of one cache head -- and a part of
-// the sequence; its four waves (eight where there is a compute unit for every workgroup) take tiles of 64 tokens in turn, each with a running maximum and sum, and are
-// joined at the end; parts are joined by a second kernel.  Nothing passes through LDS on the way in: the cache's
-// order is the one that the matrix unit wants.  With r = lane % 16, g = lane / 16:
+// the sequence; its four waves (eight where there is a compute unit for every workgroup) take tiles of 64 tokens in
+// turn, each with a running maximum and sum, and are joined at the end; parts are joined by a second kernel.  Nothing
+// passes through LDS on the way in: the cache's order is the one that the matrix unit wants.  With r = lane % 16,
+// g = lane / 16:
 //   scores: 16 tokens x 16 rows per product (16x16x32 bfloat16).  Lane (r, g) reads numbers g D/4 .. of the key of
 //     token r of a run of 16, converts them to bfloat16 (exactly: e2m1 times a power of two) and multiplies them by the same
 //     numbers of query row r.  It receives the scores of row r with tokens 4 g .. 4 g + 3 of the run.
@@ -11,13 +12,18 @@
 //     weights a lane already has: it reads piece r of those 4 tokens (16 bytes), converts, and pairs tokens by byte permutation.
 //     Lane (r, g) receives numbers 8 (4 g + i) + j of row r.
 // So a row's maximum, sum and correction are one register, the same for all of a lane's scores and results.
+// Weights are rounded to bfloat16, results of floats too: in 32 bits their product with the values, which are exact in
+// bfloat16, would be two.  The sum is that of the rounded weights.  In the norm, bfloat16 results are off by 0.0022 of themselves and by
+// 0.0017, their own rounding, with weights of 32 bits.
 // Many rows have a kernel of their own (mx4_attend_many.h).
 //
-// Bound by the reading of the cache, and by what a workgroup waits for before its first tile (lengths, table, codes, one behind the other): so
-// there are as many workgroups as the chip has at a time, and sequences of different lengths are cut into parts of one length.  32
-// sequences of up to 8191 tokens (64 query heads on 8 of 128 numbers, 183 MB) 42 us, 4.4 TB/s, the joining of parts 5 of them (parts as many for each sequence 50; the
-// same loads without the arithmetic 44 where this takes 50); one sequence of 131072 tokens (32 heads on 8) 34 us.  Codes are read with the
-// streaming hint: with caches beyond the last-level cache 50 -> 45 us, within it up to 10 % slower, and a model's caches are beyond it.
+// Bound by the reading of the cache, and by what a workgroup waits for before its first tile (lengths, table, codes,
+// one behind the other): so there are as many workgroups as the chip has at a time, and sequences of different lengths
+// are cut into parts of one length.  32 sequences of up to 8191 tokens (64 query heads on 8 of 128 numbers, 183 MB) 42
+// us where they lie in the last-level cache in part, 44 from memory (4.1 TB/s), the joining of parts 5 of them (parts as
+// many for each sequence 50; the same loads without the arithmetic 44 where this took 50); one sequence of 131072
+// tokens (32 heads on 8, 143 MB) 35 and 36 us.  Codes are read with the streaming hint: with caches beyond the last-level
+// cache 50 -> 45 us, within it up to 10 % slower, and a model's caches are beyond it.
 #include "mx4_attend_many.h"
 
 namespace gs {
@@ -194,7 +200,8 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
 #pragma unroll
       for (int p = 0; p < VP; ++p) {
         const int piece = D / 8 - 16 * p >= 16 || 16 * p + r < D / 8 ? 16 * p + r : D / 8 - 1;
-        t.v[n][p] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(w.block[n] + page * (D / 2) + w.slot[n] * (D / 2) + uint32_t(g * (D * 2) + piece * 16)));
+        const uint8_t* const codes = w.block[n] + page * (D / 2) + w.slot[n] * (D / 2) + uint32_t(g * (D * 2) + piece * 16);
+        t.v[n][p] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(codes));
         t.scale[n][p] = *reinterpret_cast<const uint32_t*>(w.block[n] + page * (D + C) + w.slot[n] * C + uint32_t(g * (C * 4) + piece / 4 * 4));
       }
   };
@@ -278,7 +285,8 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const f32x4 x = s[u][2 * h + i / 2];
-          w[u][h][i] = int32_t(pack_bf16x2(exp2_fast(fmaf(x[2 * i % 4], unit.to_log2, -ref[u])), exp2_fast(fmaf(x[2 * i % 4 + 1], unit.to_log2, -ref[u]))));
+          const float low = fmaf(x[2 * i % 4], unit.to_log2, -ref[u]), high = fmaf(x[2 * i % 4 + 1], unit.to_log2, -ref[u]);
+          w[u][h][i] = int32_t(pack_bf16x2(exp2_fast(low), exp2_fast(high)));
         }
 #pragma unroll
       for (int n = 0; n < 4; ++n) l[u] = add_weights(w[u][n / 2][2 * n % 4], w[u][n / 2][2 * n % 4 + 1], l[u]);
@@ -413,7 +421,8 @@ __global__ void __launch_bounds__(WV * 64, QT == 1 ? (D <= 128 && WV == 4 ? 3 : 
         if (D / 8 - 16 * p >= 16 || piece < D / 8)
 #pragma unroll
           for (int j = 0; j < 8; j += 4)
-            *reinterpret_cast<f32x4*>(my_o + r * kRow + piece * 8 + j) = f32x4{o[u][p][j][i], o[u][p][j + 1][i], o[u][p][j + 2][i], o[u][p][j + 3][i]};
+            *reinterpret_cast<f32x4*>(my_o + r * kRow + piece * 8 + j) =
+                f32x4{o[u][p][j][i], o[u][p][j + 1][i], o[u][p][j + 2][i], o[u][p][j + 3][i]};
       }
     __syncthreads();
     const int rr = threadIdx.x >> 4 & 15, d0 = (threadIdx.x & 15) * (D / 16);
@@ -540,17 +549,20 @@ __global__ void __launch_bounds__(256) mx4_attend_join_kernel(Mx4AttendArgs a, i
   const int32_t i = int32_t(a.by_group.div(uint32_t(row))), h = row - i * a.group;
   const int64_t dst = ((int64_t(b) * a.queries + i) * a.cache.heads * a.group + int64_t(head) * a.group + h) * D + d;
   if (a.out_dtype == GS_BF16)
-    *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + dst) = i32x2{int32_t(pack_bf16x2(x[0] * inv, x[1] * inv)), int32_t(pack_bf16x2(x[2] * inv, x[3] * inv))};
+    *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + dst) =
+        i32x2{int32_t(pack_bf16x2(x[0] * inv, x[1] * inv)), int32_t(pack_bf16x2(x[2] * inv, x[3] * inv))};
   else *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + dst) = x * inv;
 }
 
-// Row tiles of a workgroup and parts of a sequence, from sizes that the host knows (lengths may be shorter).
+// Row tiles of a workgroup and parts of a sequence, from what the host knows: the table's width stands for the lengths, which may be far
+// shorter.  A table for 131072 tokens costs 8 sequences of 700 tokens 11.7 us where one for 700 costs 8.9 (two parts and their joining), 64 of
+// 1000 20.9 and 15.4, 2048 queries of 2048 tokens 80 and 74 (rows that see different numbers of tokens in large workgroups).
 void plan(Mx4AttendArgs* a) {
   const int64_t rows = int64_t(a->queries) * a->group;
   const bool wide = a->cache.dim > 128;
-  // 256 rows per workgroup, one of them on a compute unit; 128, two of them, where most tokens are queries themselves, so that row tiles differ in
-  // what they see, and there are few (2048 queries, 32 heads of 128 numbers on 8, 78.6 and 69.6 us; 2 x 4096 of them 324 and 339; 2 x 512 over
-  // 4096 tokens 91 and 102).
+  // 256 rows per workgroup, one of them on a compute unit; 128, two of them, where most tokens are queries themselves,
+  // so that row tiles differ in what they see, and there are few (2048 queries, 32 heads of 128 numbers on 8, 78.6 and
+  // 69.6 us; 2 x 4096 of them 324 and 339; 2 x 512 over 4096 tokens 91 and 102).
   const bool uneven = a->width * a->cache.page <= 2 * int64_t(a->queries) && a->batch * a->cache.heads * ceil_div(rows, 256) <= 512;
   a->tiles = rows > 128 && !wide && !uneven ? 16 : rows > 32 ? 8 : rows > 16 ? 2 : 1;
   a->least = a->tiles >= 8 ? 4 : 8;
@@ -613,8 +625,9 @@ hipError_t launch(const Mx4AttendArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.parts > 1) {
     constexpr int kJoined = 256 / (D / 4);                // rows of a workgroup
-    if (joined_alone(a)) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(total_rows)), dim3(256), 0, s, a, int32_t(total_rows));
-    else hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, false>), dim3(unsigned(ceil_div(total_rows, kJoined))), dim3(256), 0, s, a, int32_t(total_rows));
+    const int32_t n = int32_t(total_rows);
+    if (joined_alone(a)) hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, true>), dim3(unsigned(n)), dim3(256), 0, s, a, n);
+    else hipLaunchKernelGGL((mx4_attend_join_kernel<D, kRows, false>), dim3(unsigned(ceil_div(n, kJoined))), dim3(256), 0, s, a, n);
     e = hipGetLastError();
   }
   return e;

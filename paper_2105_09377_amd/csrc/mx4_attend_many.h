@@ -9,9 +9,11 @@
 //     number, the tokens of each 16 in the order 0..3, 8..11, 4..7, 12..15, so that a lane's eight are 16 bytes.
 // Rows in LDS are an odd multiple of 16 bytes long: reads and writes of 16 rows fall on different banks.
 //
-// Bound by vector instructions (a tile of 64 numbers per head: 230 per wave, 32 of them exponentials, beside 16 products of 32 cycles): two
-// sequences' 512 queries in a window of 4096 tokens (32 heads of 64 numbers on 8) 66 us, 523 TFLOP/s; 512 over 4096 tokens of 128 numbers 91 us,
-// 569.  128 rows per workgroup, two workgroups on a compute unit: 80 and 102 us; a wave's next scores between its weights: 82 and 152 (registers).
+// Bound by vector instructions (a tile of 64 numbers per head: 230 per wave, 32 of them exponentials, beside 16 products of 32
+// cycles; 36 of them only where one of the wave's 32 rows has a new maximum, which on random scores is two tiles in five after
+// 64): two sequences' 512 queries in a window of 4096 tokens (32 heads of 64 numbers on 8) 65 to 72 us over cards, 480 to 523
+// TFLOP/s; 512 over 4096 tokens of 128 numbers 91 us, 569.  128 rows per workgroup, two workgroups on a compute unit: 80 and
+// 102 us; a wave's next scores between its weights: 82 and 152 (registers).
 #pragma once
 
 #include "mx4_span.h"
@@ -212,7 +214,8 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
 #pragma unroll
       for (int d = 0; d < NB; ++d) vf[k % 2][d] = *reinterpret_cast<const i32x4*>(values + d * 32 * kValueRow + k * 32);
     };
-    // (heads of 192 numbers: behind the last branch on scores, 512 queries over 8192 tokens 209 us, 217 from here; of 256 279 and 272)
+    // (heads of 192 numbers: behind the last branch on scores, 512 queries over 8192 tokens 211 us, 214 from here; of 256
+    // 279 and 272)
     constexpr bool kLate = D == 192;
     if constexpr (!kLate) read_values(std::integral_constant<int, 0>{});
     const bool all_seen = pages == 0x01010101u && token0 + kTile - 1 <= pos_first &&
@@ -278,7 +281,8 @@ __global__ void __launch_bounds__(64 * NW, NW == 8 || D > 128 ? 1 : 2) mx4_atten
       static_for<NB>([&](auto d_) {
         constexpr int d = decltype(d_)::value, slot = k * NB + d;
         __builtin_amdgcn_sched_barrier(0);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % 2][d]), __builtin_bit_cast(bf16x8, w[k / 2][k % 2]), o[d], 0, 0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k % 2][d]),
+                                                       __builtin_bit_cast(bf16x8, w[k / 2][k % 2]), o[d], 0, 0, 0);
         static_for<4>([&](auto i_) {
           if constexpr (decltype(i_)::value * NB / 2 == slot) weigh(std::integral_constant<int, 1>{}, i_);
         });

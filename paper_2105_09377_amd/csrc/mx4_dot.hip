@@ -25,8 +25,9 @@ typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 // ---------------------------------------------------------------------------------------------
 // Few rows of x: eight waves share a tile of 16 rows of x and 16 NT rows of w, the units of K dealt to them, their
 // partial tiles added at the end in the order of the waves.  Everything goes from memory to registers, the next unit's
-// loads in flight while one is multiplied: w is read once, and bound by that: one row with 8192 x 8192 weights 10.2 us, 3.5 TB/s from
-// a standing start (11.9 with weights that are in no cache; four units in flight 12.8, and lanes without a row of x switched off 11.8).
+// loads in flight while one is multiplied: w is read once, and bound by that: one row with 8192 x 8192 weights 12.5 us,
+// 2.9 TB/s from a standing start, 10.7 with weights that lie in the last-level cache (four units in flight 12.8, and
+// lanes without a row of x switched off 11.8, where this took 11.9).
 // ---------------------------------------------------------------------------------------------
 constexpr int kRowWaves = 8;
 template <bool XBF, int NT>
@@ -214,12 +215,14 @@ struct WeightChoice {
   Mx4DotWay way;
   int splits;
 };
-// The tile, and how many workgroups share one's sum over K (eight slabs each at least), by the time that they should take: the slabs of the
-// busiest compute unit, or what all tiles read at 10 TB/s (200 x 4096 x 11000 in 256 64x64 tiles: 456 MB, 51 us), and where sums are shared 3 us
-// for the second launch and the parts written and read, 8 bytes each at 4 TB/s.  Times that it chooses between, measured: 100 x 8192 x 8192 34.6 in 64x64 tiles, 29.6 in 64x128 by fours, 29.4 in 128x128 by fours; 200 x 8192 x 8192 53.4 in
-// 64x128, 47.4 by twos, 44.2 in 128x256 by fours; 100 x 5000 x 4104 16.9 in 64x64, 20.2 by twos; 256 x 5000 x 4104 28.6 in 64x128, 25.2 by
-// threes; 300 x 11000 x 4096 62.9 in 128x128 by twos, 53.5 in 64x64, 37.5 in 64x128; 20 x 16384 x 1024 7.0 in 32x128, 9.3 by twos; 17 x 8192 x 8192 in
-// 32x128 25.8, 17.7, 13.7 and 15.3 alone, by twos, fours and eights; 2048 x 4096 x 4096 62.8 in 128x256, 73.9 in 128x128.
+// The tile, and how many workgroups share one's sum over K (eight slabs each at least), by the time that they should
+// take: the slabs of the busiest compute unit, or what all tiles read at 10 TB/s (200 x 4096 x 11000 in 256 64x64 tiles:
+// 456 MB, 51 us), and where sums are shared 3 us for the second launch and the parts written and read, 8 bytes each at 4
+// TB/s.  Times that it chooses between, measured: 100 x 8192 x 8192 34.6 in 64x64 tiles, 29.6 in 64x128 by fours, 29.4 in
+// 128x128 by fours; 200 x 8192 x 8192 53.4 in 64x128, 47.4 by twos, 44.2 in 128x256 by fours; 100 x 5000 x 4104 16.9 in
+// 64x64, 20.2 by twos; 256 x 5000 x 4104 28.6 in 64x128, 25.2 by threes; 300 x 11000 x 4096 62.9 in 128x128 by twos, 53.5
+// in 64x64, 37.5 in 64x128; 20 x 16384 x 1024 7.0 in 32x128, 9.3 by twos; 17 x 8192 x 8192 in 32x128 25.8, 17.7, 13.7 and
+// 15.3 alone, by twos, fours and eights; 2048 x 4096 x 4096 62.8 in 128x256, 73.9 in 128x128.
 WeightChoice weight_choice(int64_t M, int64_t N, int64_t K) {
   const int32_t slabs = int32_t(ceil_div(K, 128));                 // (K is at most 2^22)
   WeightChoice best = {kWeight64x64, 1};
