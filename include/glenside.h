@@ -377,8 +377,10 @@ int glenside_mx4_cache_read(const gs_mx4_cache* cache, const gs_ap* table, const
  * A query that sees nothing, or whose scores are all -infinity, gives zeros; tokens that a query does not see
  * have no part in its result, whatever they hold.  Scores, weights and sums are fp32 (scores beyond 2.358e38, which
  * times log2(e) are infinite, count as that), weights are rounded to bf16 for their product with the values and for
- * their sum.  scale: below 2.358e38 in magnitude, for the same reason.  q ((batch, Lq, G heads),(head_dim)) bf16; out
- * of its shape and split, bf16 or f32; lengths i32 ((batch),()), taken as at least 0 and at most W P.
+ * their sum.  Weights are taken 2^-24 times as large as they are until they are divided by their sum, so that sums of
+ * the largest numbers are finite: those of values below 2^-102 lose bits.  scale: below 2.358e38 in magnitude, so that
+ * times log2(e) it is finite.  q ((batch, Lq, G heads),(head_dim)) bf16; out of its shape and split, bf16 or f32;
+ * lengths i32 ((batch),()), taken as at least 0 and at most W P.
  * workspace: glenside_mx4_attend_workspace bytes (may be 0; 16-byte aligned).                       */
 int glenside_mx4_attend(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table, const gs_ap* lengths,
                         float scale, int64_t window, int64_t sinks, gs_ap* out, void* workspace,

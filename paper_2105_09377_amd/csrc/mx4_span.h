@@ -11,7 +11,7 @@ constexpr int kTile = 64;            // tokens of a wave's step
 constexpr int kMaxParts = 64;
 constexpr int kPartHead = 4;         // floats in front of a part's results: its maximum and sum
 // Weights are 2^(score - maximum - kHeadroom): their sum over 2^24 tokens, times the largest number of the format, does not
-// overflow before it is divided by their sum.
+// overflow before it is divided by their sum.  (So values below 2^-102 are multiplied into numbers below float's normal ones.)
 constexpr float kHeadroom = 24.0f;
 
 // What the rows row0 .. row1 of a sequence of `len` tokens have to look at, in tiles: the first `sink_tiles`, then

@@ -114,3 +114,19 @@ def test_a_cache_without_pages(queries):
     for got in gs.mx4_cache_read(cache, table, n, 9):
         assert got.shape == k.shape and not got.any()
     assert not gs.mx4_attend(normal((3, queries, 4, 64), 52).to(DEV), cache, table, n, 0.1).any()
+
+
+@pytest.mark.parametrize("power,tolerance", [(-100, 2.0 ** -20), (-112, 2.0 ** -8), (-124, 2.0 ** 4)])
+@pytest.mark.parametrize("queries,group,dim", KERNELS)
+def test_attention_over_the_smallest_values(queries, group, dim, power, tolerance):
+    """Weights are 2^-24 times as large until they are divided by their sum, and a product with a value has the bits down to 2^-149: each of 60
+    is off by 2^-150 at most, 2^-126 in the result, 60 of them by less than 2^-120 in all; `tolerance` is that over the values' size."""
+    tokens = 60
+    k, v = normal((tokens, 1, dim), 61, F32), normal((tokens, 1, dim), 62, F32) * 2.0 ** power
+    cache, table = cached(k, v, 16)
+    lens = torch.tensor([tokens], dtype=torch.int32)
+    q = normal((1, queries, group, dim), 63)
+    got = to_oracle(gs.mx4_attend(q.to(DEV), cache, table.to(DEV), lens.to(DEV), dim ** -0.5, out_dtype=F32))
+    ref, mag = mx4_ways.attend(to_oracle(q), cache.data.cpu().numpy(), table.numpy(), lens.numpy(), 16, dim ** -0.5)
+    tol = (2.0 ** -8 + 2.0 ** -10) * mag + (2.0 ** -8 + 2.0 ** -20) * np.abs(ref) + tolerance * 2.0 ** power
+    assert (np.abs(got - ref) <= tol).all()
