@@ -387,6 +387,90 @@ int glenside_mx4_attend(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* 
                         size_t workspace_bytes, void* stream);
 size_t glenside_mx4_attend_workspace(const gs_ap* q, const gs_mx4_cache* cache, const gs_ap* table);
 
+/* ---------------------------------------------------------------------------------------------
+ * EXT: scaled 8-bit floats (F8).  Every access element -- its compute dimensions flattened to K numbers -- is held as
+ * B = ceil(K / 128) blocks of 128 e4m3 codes (as GS_F8 has them); codes behind K are zero:
+ *   values: ((S_A), (B, 128 bytes));
+ *   scales: floats, one for each block of one element (block_rows 1), ((S_A), (B up to a multiple of 4)), or one for
+ *           the blocks of 128 neighbouring elements (block_rows 128; along the last access dimension, whose last block may
+ *           be short): ((S_A without its last dimension, that dimension / 128 rounded up), (B up to a multiple of 4));
+ *           floats behind B are zero.
+ * A number is its code's value times its scale.                                                     */
+typedef struct {
+  void* values;               /* device pointer, 16-byte aligned, caller-owned               */
+  void* scales;               /* device pointer, 16-byte aligned, caller-owned               */
+  int32_t rank;               /* |S_A| + |S_C|, at most GS_MAX_RANK                          */
+  int32_t n_access;           /* |S_A|                                                       */
+  int32_t block_rows;         /* 1 or 128                                                    */
+  int32_t reserved;           /* must be 0                                                   */
+  int64_t shape[GS_MAX_RANK]; /* S_A ++ S_C, in numbers                                      */
+} gs_f8;
+
+/* Bytes of the two arrays of a pattern of m's shape and blocks; non-zero status if that is impossible.  Host only. */
+int glenside_f8_sizes(const gs_f8* m, size_t* values_bytes, size_t* scales_bytes);
+/* in (bf16 or f32) -> out of its shape and split.  A block's scale is max|x| times 1 / 448 (both that factor and the product
+ * rounded to float), at least 2^-126; numbers are multiplied by 1 / scale (the same) and rounded to the nearest code, ties to
+ * the even one; signs of zeros are kept.  A block with an infinity or a NaN has a scale of NaN, and zeros for codes. */
+int glenside_f8_quantize(const gs_ap* in, gs_f8* out, void* stream);
+/* The numbers as bf16 or f32, rounded once from the product of code and scale in float.            */
+int glenside_f8_dequantize(const gs_f8* in, gs_ap* out, void* stream);
+
+/* Root-mean-square norm of every access element, K numbers:
+ *   h = x + residual,   y = h / sqrt(sum h^2 / K + eps) weight.
+ * x ((a..),(c..)) bf16 or f32; residual (NULL: zeros) and sum (NULL: not wanted) of its shape, split and type; weight (NULL:
+ * ones) ((),(c..)) bf16 or f32; eps not below 0.  h is rounded to its type, and is what the norm is of: sum := h.  Squares, their sum
+ * and y are fp32: squares above float's range make the element's results zero, or NaN.
+ *   _norm    : out := y, of x's shape and split, bf16 or f32;
+ *   _f8_norm : out := y quantised as by glenside_f8_quantize (from fp32, not rounded in between), block_rows 1. */
+int glenside_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight, float eps, gs_ap* sum, gs_ap* out,
+                  void* stream);
+int glenside_f8_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight, float eps, gs_ap* sum, gs_f8* out,
+                     void* stream);
+
+/* compute dotProd (cartProd a0 a1) as glenside_cartesian_dot has it, on F8 operands of either kind of blocks: the 128
+ * products of a block are added as there (absolute error up to about 3e-5 of the sum of their magnitudes), times the product of the two
+ * scales, blocks one after the other, in fp32.  That product has to be finite (below 3.4e38; infinite, a block's results are
+ * infinite or NaN), and below 2^-126 loses bits.  out ((m.., n..),()) of bf16 or f32, act as there.  A compute shape without
+ * elements gives zeros.  Patterns of several access dimensions in blocks of 128 rows: the last one has to be a multiple of
+ * 128, or GS_ERR_UNSUPPORTED.  workspace: glenside_f8_dot_workspace bytes (may be 0; 16-byte aligned). */
+int glenside_f8_dot(const gs_f8* a0, const gs_f8* a1, gs_ap* out, int act, void* workspace, size_t workspace_bytes,
+                    void* stream);
+size_t glenside_f8_dot_workspace(const gs_f8* a0, const gs_f8* a1);
+
+/* ---------------------------------------------------------------------------------------------
+ * EXT: tokens dealt to experts.  Every one of T tokens has `choices` experts; sorted by expert, these choices are the rows of what the
+ * experts compute, and are joined again with a weight for each.
+ *
+ * _sort : experts i32 ((T, choices),()) -> offsets i32 ((E + 1),()): expert e has rows offsets[e] .. offsets[e + 1] - 1, in
+ *         the order of tokens and choices; tokens i32 ((T choices),()): the token that a row is of, -1 behind the last
+ *         row; places i32 ((T, choices),()): a choice's row, -1 where its expert is none of 0 .. E - 1 (a choice that was
+ *         dropped).  The same expert twice has two rows.  At most 4096 experts and 2^30 choices.
+ *         workspace: glenside_expert_sort_workspace(T choices, E) bytes (may be 0; 16-byte aligned).
+ * In what follows places is such a table, of any contents: a choice whose place is no row of `rows` has none.  Rows that are nobody's
+ * stay as they were.  Two choices with one place race where rows are written.
+ * _split: rows ((M),(c..)) of places[t, j] := x[t], x ((T),(c..)) of its type (any).
+ * _join : out[t] = sum_j weights[t, j] rows[places[t, j]], in fp32 in the order of j; weights f32 ((T, choices),()) (NULL:
+ *         ones, which is the gradient of _split too); rows ((M),(c..)) and out ((T),(c..)) bf16 or f32 each.
+ * _join_grad : from grad ((T),(c..)), the gradient of _join's result, those of its rows and weights:
+ *         grad_rows[places[t, j]] := weights[t, j] grad[t];  grad_weights[t, j] = sum_c grad[t, c] rows[places[t, j], c]
+ *         (f32; zero where there is no row; NULL: not wanted).  grad, rows, grad_rows of one type, bf16 or f32. */
+int glenside_expert_sort(const gs_ap* experts, gs_ap* offsets, gs_ap* tokens, gs_ap* places, void* workspace,
+                         size_t workspace_bytes, void* stream);
+size_t glenside_expert_sort_workspace(int64_t choices, int64_t n_experts);
+int glenside_expert_split(const gs_ap* x, const gs_ap* places, gs_ap* rows, void* stream);
+int glenside_expert_join(const gs_ap* rows, const gs_ap* places, const gs_ap* weights, gs_ap* out, void* stream);
+int glenside_expert_join_grad(const gs_ap* grad, const gs_ap* rows, const gs_ap* places, const gs_ap* weights,
+                              gs_ap* grad_rows, gs_ap* grad_weights, void* stream);
+/* The experts' products: out[r] = compute dotProd (cartProd a0[tokens[r]] a1[e]) for the rows r of every expert e.  a0
+ * ((T),(k..)) F8, tokens i32 ((M),()) (NULL: row r is of a0's row r, M = T; a row whose token is none of 0 .. T - 1 becomes
+ * zeros), offsets i32 ((E + 1),()) as _sort gives them, a1 ((E, N),(k..)) F8, out ((M, N),()) bf16 or f32; rows
+ * of no expert stay as they were.  Sums as in glenside_f8_dot.  Offsets are taken as at least 0, at most M, and none as below the one
+ * before; where they name a row twice, its results race.
+ * workspace: glenside_f8_expert_dot_workspace(a0, M, a1) bytes (may be 0; 16-byte aligned).           */
+int glenside_f8_expert_dot(const gs_f8* a0, const gs_ap* tokens, const gs_ap* offsets, const gs_f8* a1, gs_ap* out,
+                           int act, void* workspace, size_t workspace_bytes, void* stream);
+size_t glenside_f8_expert_dot_workspace(const gs_f8* a0, int64_t rows, const gs_f8* a1);
+
 #ifdef __cplusplus
 }
 #endif

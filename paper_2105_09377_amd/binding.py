@@ -42,6 +42,9 @@ EXPORTS = (
     "glenside_mx4_sizes", "glenside_mx4_quantize", "glenside_mx4_dequantize", "glenside_mx4_dot", "glenside_mx4_dot_workspace",
     "glenside_mx4_weight_dot", "glenside_mx4_weight_dot_workspace", "glenside_mx4_cache_bytes", "glenside_mx4_cache_append",
     "glenside_mx4_cache_read", "glenside_mx4_attend", "glenside_mx4_attend_workspace",
+    "glenside_f8_sizes", "glenside_f8_quantize", "glenside_f8_dequantize", "glenside_norm", "glenside_f8_norm", "glenside_f8_dot",
+    "glenside_f8_dot_workspace", "glenside_f8_expert_dot", "glenside_f8_expert_dot_workspace", "glenside_expert_sort",
+    "glenside_expert_sort_workspace", "glenside_expert_split", "glenside_expert_join", "glenside_expert_join_grad",
 )
 
 
@@ -59,6 +62,11 @@ class gs_mx4(ctypes.Structure):
 class gs_mx4_cache(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class gs_f8(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rank", ctypes.c_int32), ("n_access", ctypes.c_int32),
+                ("block_rows", ctypes.c_int32), ("reserved", ctypes.c_int32), ("shape", ctypes.c_int64 * GS_MAX_RANK)]
 
 
 class gs_named_ap(ctypes.Structure):
@@ -138,8 +146,24 @@ def lib() -> ctypes.CDLL:
         L.glenside_mx4_cache_read.argtypes = [cache_p, ap_p, ap_p, ap_p, ap_p, vp]
         L.glenside_mx4_attend.argtypes = [ap_p, cache_p, ap_p, ap_p, ctypes.c_float, ctypes.c_int64, ctypes.c_int64, ap_p, vp, size, vp]
         L.glenside_mx4_attend_workspace.argtypes = [ap_p, cache_p, ap_p]
+        f8_p, i64 = ctypes.POINTER(gs_f8), ctypes.c_int64
+        L.glenside_f8_sizes.argtypes = [f8_p, size_p, size_p]
+        L.glenside_f8_quantize.argtypes = [ap_p, f8_p, vp]
+        L.glenside_f8_dequantize.argtypes = [f8_p, ap_p, vp]
+        L.glenside_norm.argtypes = [ap_p, ap_p, ap_p, ctypes.c_float, ap_p, ap_p, vp]
+        L.glenside_f8_norm.argtypes = [ap_p, ap_p, ap_p, ctypes.c_float, ap_p, f8_p, vp]
+        L.glenside_f8_dot.argtypes = [f8_p, f8_p, ap_p, ctypes.c_int, vp, size, vp]
+        L.glenside_f8_dot_workspace.argtypes = [f8_p, f8_p]
+        L.glenside_f8_expert_dot.argtypes = [f8_p, ap_p, ap_p, f8_p, ap_p, ctypes.c_int, vp, size, vp]
+        L.glenside_f8_expert_dot_workspace.argtypes = [f8_p, i64, f8_p]
+        L.glenside_expert_sort.argtypes = [ap_p, ap_p, ap_p, ap_p, vp, size, vp]
+        L.glenside_expert_sort_workspace.argtypes = [i64, i64]
+        L.glenside_expert_split.argtypes = [ap_p, ap_p, ap_p, vp]
+        L.glenside_expert_join.argtypes = [ap_p, ap_p, ap_p, ap_p, vp]
+        L.glenside_expert_join_grad.argtypes = [ap_p, ap_p, ap_p, ap_p, ap_p, ap_p, vp]
         for f in (L.glenside_mx4_dot_workspace, L.glenside_mx4_weight_dot_workspace, L.glenside_mx4_cache_bytes,
-                  L.glenside_mx4_attend_workspace):
+                  L.glenside_mx4_attend_workspace, L.glenside_f8_dot_workspace, L.glenside_f8_expert_dot_workspace,
+                  L.glenside_expert_sort_workspace):
             f.restype = size
         _bind_native(L)
         _lib = L
@@ -538,3 +562,101 @@ def mx4_attend(q: torch.Tensor, cache: Mx4Cache, table: torch.Tensor, lengths: t
     """Attention of the last queries q (batch, Lq, heads, head_dim) of every sequence over its lengths[b] cached tokens,
     causal, over a sliding window with the first `sinks` tokens kept where `window` is not zero."""
     return _m().mx4_attend(q, cache, table, lengths, scale, window, sinks, out_dtype, out, workspace)
+
+
+# ---------------------------------------------------------------------------------------------
+# scaled 8-bit floats (F8): blocks of 128 e4m3 numbers of one row, or of 128 rows, with a float scale; norms
+# ---------------------------------------------------------------------------------------------
+
+
+class F8(NamedTuple):
+    """An access pattern held in F8: `values` S_A ++ (blocks, 128), float8_e4m3fn or bytes, and `scales` in float32, S_A ++ (blocks up to a
+    multiple of 4), the last access dimension divided by `block_rows` (1 or 128); the numbers' shape S_A ++ S_C and |S_A|."""
+    values: torch.Tensor
+    scales: torch.Tensor
+    shape: Tuple[int, ...]
+    n_access: int
+    block_rows: int = 1
+
+
+def f8_quantize(x: torch.Tensor, n_access: Optional[int] = None, block_rows: int = 1, out: Optional[F8] = None) -> F8:
+    """The numbers of (access x n_access), bfloat16 or float32, in F8; n_access is the last dimension by default.  `block_rows` is
+    1 for what is multiplied row by row (activations), 128 for matrices that stay (weights); `out` has its own."""
+    n = x.dim() - 1 if n_access is None else n_access
+    pair = _m().f8_quantize(x, n, block_rows, out)
+    return out if out is not None else F8(pair[0], pair[1], tuple(x.shape), n, block_rows)
+
+
+def f8_dequantize(m: F8, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The numbers as bfloat16 (default) or float32."""
+    return _m().f8_dequantize(m, out_dtype, out)
+
+
+def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+         n_access: Optional[int] = None, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+         total: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Root-mean-square norm of x + residual over (access x n_access)'s compute dimensions, times weight: (the norm, of x's type by
+    default; the sum, which is x itself where there is no residual)."""
+    n = x.dim() - 1 if n_access is None else n_access
+    return _m().norm(False, x, weight, residual, eps, n, out_dtype, out, total)
+
+
+def f8_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+            n_access: Optional[int] = None, out: Optional[F8] = None, total: Optional[torch.Tensor] = None) -> Tuple[F8, torch.Tensor]:
+    """`norm` with its result in F8, rounded once."""
+    n = x.dim() - 1 if n_access is None else n_access
+    values, scales, total = _m().norm(True, x, weight, residual, eps, n, None, out, total)
+    return (out if out is not None else F8(values, scales, tuple(x.shape), n, 1)), total
+
+
+def f8_dot(a0: F8, a1: F8, out_dtype: Optional[torch.dtype] = None, act: int = GS_ACT_NONE, out: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """compute dotProd (cartProd a0 a1) of two F8 patterns -> float32 (default) or bfloat16 of shape S_A(a0) ++ S_A(a1)."""
+    return _m().f8_dot(a0, a1, out_dtype, act, out, workspace)
+
+
+# ---------------------------------------------------------------------------------------------
+# tokens dealt to experts
+# ---------------------------------------------------------------------------------------------
+
+
+class ExpertSort(NamedTuple):
+    """Choices sorted by expert: expert e has rows offsets[e] .. offsets[e + 1] - 1; each row's token, -1 behind the last; each choice's
+    row, -1 where it was dropped."""
+    offsets: torch.Tensor
+    tokens: torch.Tensor
+    places: torch.Tensor
+
+
+def expert_sort(experts: torch.Tensor, n_experts: int, out: Optional[ExpertSort] = None,
+                workspace: Optional[torch.Tensor] = None) -> ExpertSort:
+    """Rows for the experts (tokens, choices), int32, of every token; a choice that is none of 0 .. n_experts - 1 is dropped."""
+    three = _m().expert_sort(experts, n_experts, out, workspace)
+    return out if out is not None else ExpertSort(*three)
+
+
+def expert_split(x: torch.Tensor, places: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tokens x (tokens, ..) -> rows, every token at the places of its choices; rows that are nobody's stay as they were."""
+    return _m().expert_split(x, places, out)
+
+
+def expert_join(rows: torch.Tensor, places: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows -> tokens (tokens, ..): the sum of every token's rows, times weights (tokens, choices) in float32.  Without weights it is
+    the gradient of `expert_split` too."""
+    return _m().expert_join(rows, places, weights, out_dtype, out)
+
+
+def expert_join_grad(grad: torch.Tensor, rows: torch.Tensor, places: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                     grad_rows: Optional[torch.Tensor] = None,
+                     grad_weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The gradients of `expert_join`'s rows and weights, of the gradient of its result; gradients of rows that are nobody's stay as they
+    were."""
+    return _m().expert_join_grad(grad, rows, places, weights, grad_rows, grad_weights)
+
+
+def f8_expert_dot(a0: F8, w: F8, offsets: torch.Tensor, tokens: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                  act: int = GS_ACT_NONE, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Row r -> a0's row tokens[r] (r without tokens) times the matrix of w ((experts, n), (k)) whose expert has row r by `offsets`;
+    rows of no expert stay as they were."""
+    return _m().f8_expert_dot(a0, w, offsets, tokens, out_dtype, act, out, workspace)

@@ -1,0 +1,72 @@
+// Which rows of the result a workgroup has.
+#pragma once
+
+#include "f8.h"
+
+namespace gs {
+
+namespace {
+
+struct F8Rows {
+  int64_t first, end;                  // rows of the result; none where end is not above first
+  int64_t expert;
+};
+
+// Sums over the lanes up to and with this one.
+__device__ __forceinline__ int32_t lanes_up_to(int32_t v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int32_t o = __shfl_up(v, d);
+    v += lane >= d ? o : 0;
+  }
+  return v;
+}
+
+// Expert e's rows of M, whatever the offsets are.
+__device__ __forceinline__ void f8_rows_of(const F8DotArgs& a, int64_t e, int64_t* lo, int64_t* hi) {
+  const int64_t l = a.offsets[e], h = a.offsets[e + 1];
+  *lo = l < 0 ? 0 : l < a.M ? l : a.M;
+  *hi = h < *lo ? *lo : h < a.M ? h : a.M;
+}
+
+// The tile-th of the tiles of `size` rows that experts' rows are cut into, expert by expert; every wave finds it by itself.
+// *all: their number, where the tile is none of them.
+__device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile, int size, int64_t* all) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int64_t e0 = 0; e0 < a.experts; e0 += 64) {
+    const int64_t e = e0 + lane;
+    int64_t lo = 0, hi = 0;
+    if (e < a.experts) f8_rows_of(a, e, &lo, &hi);
+    const int32_t tiles = int32_t((hi - lo + size - 1) / size);
+    const int32_t upto = lanes_up_to(tiles, lane);
+    const uint64_t behind = __ballot(before + upto > tile);
+    if (behind) {
+      const int first = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)behind) - 1);
+      F8Rows r;
+      const int64_t row = lo + (tile - before - (upto - tiles)) * size;
+      const int32_t row32 = __builtin_amdgcn_readlane(int32_t(row), first), lo32 = __builtin_amdgcn_readlane(int32_t(lo), first),
+                    hi32 = __builtin_amdgcn_readlane(int32_t(hi), first);
+      r.first = row32;
+      r.end = hi32;
+      // (offsets that go down could give a number of tiles that has overflowed)
+      if (row32 < lo32) r.end = r.first;
+      r.expert = e0 + first;
+      return r;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  *all = before;
+  return F8Rows{0, 0, 0};
+}
+
+// The row of x that a row of the result is of, -1 where there is none.
+__device__ __forceinline__ int64_t f8_x_row(const F8DotArgs& a, int64_t row) {
+  if (!a.tokens) return row;
+  const int64_t t = a.tokens[row];
+  return t >= 0 && t < a.x_count ? t : -1;
+}
+
+}  // namespace
+
+}  // namespace gs

@@ -49,6 +49,20 @@ struct Api {
   decltype(&glenside_mx4_cache_read) mx4_cache_read;
   decltype(&glenside_mx4_attend) mx4_attend;
   decltype(&glenside_mx4_attend_workspace) mx4_attend_workspace;
+  decltype(&glenside_f8_sizes) f8_sizes;
+  decltype(&glenside_f8_quantize) f8_quantize;
+  decltype(&glenside_f8_dequantize) f8_dequantize;
+  decltype(&glenside_norm) norm;
+  decltype(&glenside_f8_norm) f8_norm;
+  decltype(&glenside_f8_dot) f8_dot;
+  decltype(&glenside_f8_dot_workspace) f8_dot_workspace;
+  decltype(&glenside_f8_expert_dot) f8_expert_dot;
+  decltype(&glenside_f8_expert_dot_workspace) f8_expert_dot_workspace;
+  decltype(&glenside_expert_sort) expert_sort;
+  decltype(&glenside_expert_sort_workspace) expert_sort_workspace;
+  decltype(&glenside_expert_split) expert_split;
+  decltype(&glenside_expert_join) expert_join;
+  decltype(&glenside_expert_join_grad) expert_join_grad;
 } api;
 PyObject* error_class;
 
@@ -533,7 +547,7 @@ PyObject* py_program_eval(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // Storage of one byte per element, dense.
 void* bytes_of(const at::Tensor& t) {
   if (t.element_size() != 1 || !t.is_contiguous()) {
-    PyErr_SetString(PyExc_ValueError, "4-bit numbers, their scales and caches are dense tensors of bytes");
+    PyErr_SetString(PyExc_ValueError, "4-bit and 8-bit numbers, scales of 4-bit ones, caches and workspaces are dense tensors of bytes");
     throw Failed{};
   }
   return t.data_ptr();
@@ -758,6 +772,269 @@ PyObject* py_mx4_attend(PyObject*, PyObject* const* p, Py_ssize_t n) {
   });
 }
 
+// binding.F8: (values, scales, shape, n_access, block_rows)
+struct F8 {
+  at::Tensor values, scales;
+  gs_f8 d{};
+  explicit F8(PyObject* o) : values(tensor(item(o, 0, 5, "an F8"))), scales(tensor(item(o, 1, 5, "an F8"))) {
+    d.values = bytes_of(values);
+    if (scales.scalar_type() != at::kFloat || !scales.is_contiguous()) {
+      PyErr_SetString(PyExc_ValueError, "scales are dense tensors of float32");
+      throw Failed{};
+    }
+    d.scales = scales.data_ptr();
+    const Ints shape(item(o, 2, 5, "an F8"));
+    pattern(shape.v, shape.n, integer(item(o, 3, 5, "an F8")), integer(item(o, 4, 5, "an F8")));
+    size_t need_values = 0, need_scales = 0;
+    call("f8_sizes", [&] { return api.f8_sizes(&d, &need_values, &need_scales); });
+    if (size_t(values.numel()) < need_values || size_t(scales.numel()) * 4 < need_scales) refuse(GS_ERR_SHAPE, "F8");
+    same_device(values, {&scales});
+  }
+  // New storage for a pattern.
+  F8(const int64_t* shape, int64_t rank, int64_t n_access, int64_t block_rows, const at::Tensor& like) {
+    pattern(shape, rank, n_access, block_rows);
+    size_t need_values = 0, need_scales = 0;
+    call("f8_sizes", [&] { return api.f8_sizes(&d, &need_values, &need_scales); });
+    int64_t cols = 1, v[GS_MAX_RANK + 2];
+    for (int64_t i = n_access; i < rank; ++i) cols *= shape[i];
+    for (int64_t i = 0; i < n_access; ++i) v[i] = shape[i];
+    v[n_access] = (cols + 127) / 128;
+    v[n_access + 1] = 128;
+    values = at::empty(at::IntArrayRef(v, size_t(n_access) + 2), at::TensorOptions().dtype(at::kFloat8_e4m3fn).device(like.device()));
+    if (n_access > 0) v[n_access - 1] = (v[n_access - 1] + block_rows - 1) / block_rows;
+    v[n_access] = (v[n_access] + 3) / 4 * 4;
+    scales = at::empty(at::IntArrayRef(v, size_t(n_access) + 1), at::TensorOptions().dtype(at::kFloat).device(like.device()));
+    d.values = values.data_ptr();
+    d.scales = scales.data_ptr();
+  }
+
+ private:
+  void pattern(const int64_t* shape, int64_t rank, int64_t n_access, int64_t block_rows) {
+    if (rank > GS_MAX_RANK) {
+      PyErr_SetString(PyExc_ValueError, "rank above GS_MAX_RANK");
+      throw Failed{};
+    }
+    if (n_access < 0 || n_access > rank) refuse(GS_ERR_RANK, "F8");
+    if (block_rows != 1 && block_rows != 128) refuse(GS_ERR_UNSUPPORTED, "F8");
+    d.rank = int32_t(rank);
+    d.n_access = int32_t(n_access);
+    d.block_rows = int32_t(block_rows);
+    for (int64_t i = 0; i < rank; ++i) d.shape[i] = shape[i];
+  }
+};
+
+at::Tensor optional_tensor(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
+
+// f8_quantize(x, n_access, block_rows, out) -> (values, scales); out: an F8 or None
+PyObject* py_f8_quantize(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 4, [&](PyObject*& r) {
+    const at::Tensor& x = tensor(p[0]);
+    const gs_ap xa = describe(x, integer(p[1]));
+    F8 out = p[3] == Py_None ? F8(xa.shape, xa.rank, xa.n_access, integer(p[2]), x) : F8(p[3]);
+    same_device(x, {&out.values});
+    void* s = stream_of(x);
+    call("f8_quantize", [&] { return api.f8_quantize(&xa, &out.d, s); });
+    const Owned values(THPVariable_Wrap(out.values)), scales(THPVariable_Wrap(out.scales));
+    r = PyTuple_Pack(2, values.object, scales.object);
+    if (!r) throw Failed{};
+  });
+}
+
+// f8_dequantize(m, out_dtype, out)
+PyObject* py_f8_dequantize(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 3, [&](PyObject*& r) {
+    const F8 m(p[0]);
+    Result out(p[2], p[1], at::kBFloat16, m.d.shape, m.d.rank, m.values);
+    r = out.object;
+    gs_ap oa = describe(out.value, m.d.n_access);
+    same_device(m.values, {&out.value});
+    void* s = stream_of(m.values);
+    call("f8_dequantize", [&] { return api.f8_dequantize(&m.d, &oa, s); });
+  });
+}
+
+// norm(f8, x, weight, residual, eps, n_access, out_dtype, out, sum) -> f8: (values, scales, sum), else (out, sum); sum is
+// x itself where there is no residual and no tensor for it is given
+PyObject* py_norm(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 9, [&](PyObject*& r) {
+    const bool f8 = p[0] == Py_True;
+    const at::Tensor& x = tensor(p[1]);
+    const at::Tensor weight = optional_tensor(p[2]), residual = optional_tensor(p[3]);
+    const double eps = PyFloat_AsDouble(p[4]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Failed{};
+    const gs_ap xa = describe(x, integer(p[5]));
+    gs_ap wa{}, ra{}, sa{};
+    if (weight.defined()) wa = describe(weight, 0);
+    if (residual.defined()) ra = describe(residual, xa.n_access);
+    at::Tensor sum;
+    if (p[8] != Py_None) sum = tensor(p[8]);
+    else if (residual.defined()) sum = at::empty(x.sizes(), x.options());
+    if (sum.defined()) sa = describe(sum, xa.n_access);
+    same_device(x, {&weight, &residual, &sum});
+    void* s = stream_of(x);
+    const gs_ap *w = weight.defined() ? &wa : nullptr, *res = residual.defined() ? &ra : nullptr;
+    gs_ap* total = sum.defined() ? &sa : nullptr;
+    const Owned total_held(THPVariable_Wrap(sum.defined() ? sum : x));
+    if (f8) {
+      F8 out = p[7] == Py_None ? F8(xa.shape, xa.rank, xa.n_access, 1, x) : F8(p[7]);
+      same_device(x, {&out.values});
+      call("f8_norm", [&] { return api.f8_norm(&xa, res, w, float(eps), total, &out.d, s); });
+      const Owned values(THPVariable_Wrap(out.values)), scales(THPVariable_Wrap(out.scales));
+      r = PyTuple_Pack(3, values.object, scales.object, total_held.object);
+    } else {
+      const Result out(p[7], p[6], x.scalar_type(), xa.shape, xa.rank, x);
+      const Owned out_held(out.object);
+      same_device(x, {&out.value});
+      gs_ap oa = describe(out.value, xa.n_access);
+      call("norm", [&] { return api.norm(&xa, res, w, float(eps), total, &oa, s); });
+      r = PyTuple_Pack(2, out.object, total_held.object);
+    }
+    if (!r) throw Failed{};
+  });
+}
+
+// f8_dot(a0, a1, out_dtype, act, out, workspace)
+PyObject* py_f8_dot(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 6, [&](PyObject*& r) {
+    const F8 a0(p[0]), a1(p[1]);
+    const int act = code(p[3]);
+    int64_t shape[2 * GS_MAX_RANK];
+    int rank = 0;
+    for (int i = 0; i < a0.d.n_access; ++i) shape[rank++] = a0.d.shape[i];
+    for (int i = 0; i < a1.d.n_access; ++i) shape[rank++] = a1.d.shape[i];
+    Result out(p[4], p[2], at::kFloat, shape, rank, a0.values);
+    r = out.object;
+    gs_ap oa = describe_all(out.value);
+    const at::Tensor ws = workspace_for(p[5], p[5] == Py_None ? api.f8_dot_workspace(&a0.d, &a1.d) : 0, a0.values);
+    same_device(a0.values, {&a1.values, &out.value, &ws});
+    void *s = stream_of(a0.values), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("f8_dot", [&] { return api.f8_dot(&a0.d, &a1.d, &oa, act, w, bytes, s); });
+  });
+}
+
+// f8_expert_dot(a0, w, offsets, tokens, out_dtype, act, out, workspace)
+PyObject* py_f8_expert_dot(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 8, [&](PyObject*& r) {
+    const F8 a0(p[0]), a1(p[1]);
+    const at::Tensor& offsets = tensor(p[2]);
+    const at::Tensor tokens = optional_tensor(p[3]);
+    const int act = code(p[5]);
+    if (tokens.defined() && tokens.dim() != 1) refuse(GS_ERR_RANK, "f8_expert_dot");
+    int64_t shape[2] = {1, a1.d.n_access > 0 ? a1.d.shape[a1.d.n_access - 1] : 1};
+    if (tokens.defined()) shape[0] = tokens.size(0);
+    else
+      for (int i = 0; i < a0.d.n_access; ++i) shape[0] *= a0.d.shape[i];
+    Result out(p[6], p[4], at::kFloat, shape, 2, a0.values);
+    r = out.object;
+    const gs_ap fa = describe(offsets, 1);
+    gs_ap ta{}, oa = describe_all(out.value);
+    if (tokens.defined()) ta = describe(tokens, 1);
+    const at::Tensor ws = workspace_for(p[7], p[7] == Py_None ? api.f8_expert_dot_workspace(&a0.d, shape[0], &a1.d) : 0, a0.values);
+    same_device(a0.values, {&a1.values, &offsets, &tokens, &out.value, &ws});
+    void *s = stream_of(a0.values), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("f8_expert_dot", [&] { return api.f8_expert_dot(&a0.d, tokens.defined() ? &ta : nullptr, &fa, &a1.d, &oa, act, w, bytes, s); });
+  });
+}
+
+// expert_sort(experts, n_experts, out, workspace) -> (offsets, tokens, places); out: three tensors or None
+PyObject* py_expert_sort(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 4, [&](PyObject*& r) {
+    const at::Tensor& experts = tensor(p[0]);
+    const int64_t n_experts = integer(p[1]);
+    if (n_experts < 0 || n_experts > (int64_t(1) << 30)) refuse(GS_ERR_SHAPE, "expert_sort");
+    at::Tensor offsets, tokens, places;
+    if (p[2] != Py_None) {
+      offsets = tensor(item(p[2], 0, 3, "an ExpertSort"));
+      tokens = tensor(item(p[2], 1, 3, "an ExpertSort"));
+      places = tensor(item(p[2], 2, 3, "an ExpertSort"));
+      if (offsets.dim() == 1 && offsets.size(0) != n_experts + 1) refuse(GS_ERR_SHAPE, "expert_sort");
+    } else {
+      const auto ints = at::TensorOptions().dtype(at::kInt).device(experts.device());
+      offsets = at::empty({n_experts + 1}, ints);
+      tokens = at::empty({experts.numel()}, ints);
+      places = at::empty(experts.sizes(), ints);
+    }
+    const gs_ap ea = describe_all(experts);
+    gs_ap oa = describe_all(offsets), ta = describe_all(tokens), pa = describe_all(places);
+    const at::Tensor ws = workspace_for(p[3], p[3] == Py_None ? api.expert_sort_workspace(experts.numel(), n_experts) : 0, experts);
+    same_device(experts, {&offsets, &tokens, &places, &ws});
+    void *s = stream_of(experts), *w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? size_t(ws.numel()) : 0;
+    call("expert_sort", [&] { return api.expert_sort(&ea, &oa, &ta, &pa, w, bytes, s); });
+    const Owned o(THPVariable_Wrap(offsets)), t(THPVariable_Wrap(tokens)), q(THPVariable_Wrap(places));
+    r = PyTuple_Pack(3, o.object, t.object, q.object);
+    if (!r) throw Failed{};
+  });
+}
+
+// A shape like `of`'s with another first dimension.
+struct RowsShape {
+  int64_t v[GS_MAX_RANK];
+  int rank;
+  RowsShape(const at::Tensor& of, int64_t first) : rank(int(of.dim())) {
+    if (rank < 1 || rank > GS_MAX_RANK) {
+      PyErr_SetString(PyExc_ValueError, "tokens and rows have 1 to 8 dimensions");
+      throw Failed{};
+    }
+    for (int i = 0; i < rank; ++i) v[i] = i ? of.size(i) : first;
+  }
+};
+
+// expert_split(x, places, out)
+PyObject* py_expert_split(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 3, [&](PyObject*& r) {
+    const at::Tensor &x = tensor(p[0]), &places = tensor(p[1]);
+    const RowsShape shape(x, places.numel());
+    Result rows(p[2], Py_None, x.scalar_type(), shape.v, shape.rank, x);
+    r = rows.object;
+    const gs_ap xa = describe(x, 1), pa = describe_all(places);
+    gs_ap ra = describe(rows.value, 1);
+    same_device(x, {&places, &rows.value});
+    void* s = stream_of(x);
+    call("expert_split", [&] { return api.expert_split(&xa, &pa, &ra, s); });
+  });
+}
+
+// expert_join(rows, places, weights, out_dtype, out)
+PyObject* py_expert_join(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 5, [&](PyObject*& r) {
+    const at::Tensor &rows = tensor(p[0]), &places = tensor(p[1]);
+    const at::Tensor weights = optional_tensor(p[2]);
+    const RowsShape shape(rows, places.dim() ? places.size(0) : 0);
+    Result out(p[4], p[3], rows.scalar_type(), shape.v, shape.rank, rows);
+    r = out.object;
+    const gs_ap ra = describe(rows, 1), pa = describe_all(places);
+    gs_ap wa{}, oa = describe(out.value, 1);
+    if (weights.defined()) wa = describe_all(weights);
+    same_device(rows, {&places, &weights, &out.value});
+    void* s = stream_of(rows);
+    call("expert_join", [&] { return api.expert_join(&ra, &pa, weights.defined() ? &wa : nullptr, &oa, s); });
+  });
+}
+
+// expert_join_grad(grad, rows, places, weights, grad_rows, grad_weights) -> (grad_rows, grad_weights)
+PyObject* py_expert_join_grad(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded(n, 6, [&](PyObject*& r) {
+    const at::Tensor &grad = tensor(p[0]), &rows = tensor(p[1]), &places = tensor(p[2]);
+    const at::Tensor weights = optional_tensor(p[3]);
+    const RowsShape shape(rows, rows.dim() ? rows.size(0) : 0);
+    const Result grad_rows(p[4], Py_None, rows.scalar_type(), shape.v, shape.rank, rows);
+    const Owned rows_held(grad_rows.object);
+    const Result grad_weights(p[5], Py_None, at::kFloat, places.sizes().data(), int(places.dim()), rows);
+    const Owned weights_held(grad_weights.object);
+    const gs_ap ga = describe(grad, 1), ra = describe(rows, 1), pa = describe_all(places);
+    gs_ap wa{}, gra = describe(grad_rows.value, 1), gwa = describe_all(grad_weights.value);
+    if (weights.defined()) wa = describe_all(weights);
+    same_device(grad, {&rows, &places, &weights, &grad_rows.value, &grad_weights.value});
+    void* s = stream_of(grad);
+    call("expert_join_grad", [&] { return api.expert_join_grad(&ga, &ra, &pa, weights.defined() ? &wa : nullptr, &gra, &gwa, s); });
+    r = PyTuple_Pack(2, grad_rows.object, grad_weights.object);
+    if (!r) throw Failed{};
+  });
+}
+
 // bind(addresses by entry point name, GlensideError)
 PyObject* py_bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded(n, 2, [&](PyObject*& r) {
@@ -802,6 +1079,20 @@ PyObject* py_bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
     get("glenside_mx4_cache_read", api.mx4_cache_read);
     get("glenside_mx4_attend", api.mx4_attend);
     get("glenside_mx4_attend_workspace", api.mx4_attend_workspace);
+    get("glenside_f8_sizes", api.f8_sizes);
+    get("glenside_f8_quantize", api.f8_quantize);
+    get("glenside_f8_dequantize", api.f8_dequantize);
+    get("glenside_norm", api.norm);
+    get("glenside_f8_norm", api.f8_norm);
+    get("glenside_f8_dot", api.f8_dot);
+    get("glenside_f8_dot_workspace", api.f8_dot_workspace);
+    get("glenside_f8_expert_dot", api.f8_expert_dot);
+    get("glenside_f8_expert_dot_workspace", api.f8_expert_dot_workspace);
+    get("glenside_expert_sort", api.expert_sort);
+    get("glenside_expert_sort_workspace", api.expert_sort_workspace);
+    get("glenside_expert_split", api.expert_split);
+    get("glenside_expert_join", api.expert_join);
+    get("glenside_expert_join_grad", api.expert_join_grad);
     Py_INCREF(p[1]);
     Py_XDECREF(error_class);
     error_class = p[1];
@@ -819,6 +1110,9 @@ PyMethodDef methods[] = {
     GS_FN("mx4_quantize", py_mx4_quantize), GS_FN("mx4_dequantize", py_mx4_dequantize), GS_FN("mx4_dot", py_mx4_dot),
     GS_FN("mx4_weight_dot", py_mx4_weight_dot), GS_FN("mx4_cache_append", py_mx4_cache_append),
     GS_FN("mx4_cache_read", py_mx4_cache_read), GS_FN("mx4_attend", py_mx4_attend),
+    GS_FN("f8_quantize", py_f8_quantize), GS_FN("f8_dequantize", py_f8_dequantize), GS_FN("norm", py_norm), GS_FN("f8_dot", py_f8_dot),
+    GS_FN("f8_expert_dot", py_f8_expert_dot), GS_FN("expert_sort", py_expert_sort), GS_FN("expert_split", py_expert_split),
+    GS_FN("expert_join", py_expert_join), GS_FN("expert_join_grad", py_expert_join_grad),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
