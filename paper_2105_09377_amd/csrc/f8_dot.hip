@@ -4,17 +4,11 @@
 // The matrix unit multiplies the 128 codes of a block (16x16x128: one instruction), into zeros; the block's sum, times the product of
 // the two scales, is added to the result by vector instructions.  w is the operand whose rows become rows of a lane's results, x the one
 // that becomes columns: a lane's results are all of one row of x, so that it needs one scale of x for each block.
-#include "f8_group.h"
+#include "f8_tile.h"
 
 namespace gs {
 
 namespace {
-
-__device__ __forceinline__ f32x4 f8_mfma16(const i32x4 (&w)[2], const i32x4 (&x)[2]) {
-  const i32x8 a = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
-  const i32x8 b = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-}
 
 // ---------------------------------------------------------------------------------------------
 // Few rows: eight waves share a tile of 16 rows of x and 16 NT rows of w, the blocks of K dealt to them four at a time (16 bytes
@@ -29,8 +23,7 @@ __global__ void __launch_bounds__(kRowWaves * 64) f8_dot_rows_kernel(F8DotArgs a
   const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
   F8Rows rows = {int64_t(tm) * 16, a.M, 0};
   if constexpr (GROUPED) {
-    int64_t all;
-    rows = f8_group_tile(a, tm, 16, &all);
+    rows = f8_group_tile(a, tm, 16);
     if (rows.end <= rows.first) return;
   }
   const int64_t m0 = rows.first, n0 = int64_t(tn) * 16 * NT;
@@ -112,13 +105,35 @@ hipError_t launch_rows(const F8DotArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+enum F8DotWay { kF8Rows, kF8Tile256x256, kF8Tile128x128, kF8Tile64x64 };
+
+int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * ceil_div(N, bn); }
+
 }  // namespace
 
-F8DotPlan plan_f8_dot(int64_t, int64_t, int64_t, int64_t) { return F8DotPlan{0, 1, 0}; }
+F8DotPlan plan_f8_dot(int64_t M, int64_t N, int64_t K, int64_t experts) {
+  F8DotPlan p = {kF8Rows, 1, 0};
+  if (K == 0 || K > (int64_t(1) << 22)) return p;
+  const int64_t rows = experts ? ceil_div(M, experts) : M;     // of a matrix
+  if (rows <= 16) return p;
+  if (tiles(M, N, 256, 256) >= 180) p.way = kF8Tile256x256;
+  else if (tiles(M, N, 128, 128) >= 192) p.way = kF8Tile128x128;
+  else p.way = kF8Tile64x64;
+  return p;
+}
 
-hipError_t launch_f8_dot(const F8DotArgs& a, const F8DotPlan&, void*, hipStream_t s) {
+hipError_t launch_f8_dot(const F8DotArgs& given, const F8DotPlan& plan, void*, hipStream_t s) {
+  F8DotArgs a = given;
   if (a.M == 0 || a.N == 0) return hipSuccess;
-  return launch_rows<2>(a, s);
+  a.splits = 1;
+  // (rows of x that experts share are found by 32-bit offsets in tiles)
+  const bool far = a.offsets && a.K > 0 && a.x_count > int64_t(0xffffffffu) / a.K;
+  switch (far ? kF8Rows : plan.way) {
+    case kF8Tile256x256: return launch_f8_tiles<256, 256, 4, 2, 2>(a, most_tiles(a, 256), s);
+    case kF8Tile128x128: return launch_f8_tiles<128, 128, 2, 2, 2>(a, most_tiles(a, 128), s);
+    case kF8Tile64x64: return launch_f8_tiles<64, 64, 2, 2, 4>(a, most_tiles(a, 64), s);
+    default: return launch_rows<2>(a, s);
+  }
 }
 
 }  // namespace gs

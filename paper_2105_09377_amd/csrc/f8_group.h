@@ -29,9 +29,21 @@ __device__ __forceinline__ void f8_rows_of(const F8DotArgs& a, int64_t e, int64_
   *hi = h < *lo ? *lo : h < a.M ? h : a.M;
 }
 
-// The tile-th of the tiles of `size` rows that experts' rows are cut into, expert by expert; every wave finds it by itself.
-// *all: their number, where the tile is none of them.
-__device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile, int size, int64_t* all) {
+// How many tiles of `size` rows the experts' rows are cut into, expert by expert.
+__device__ __forceinline__ int64_t f8_group_tiles(const F8DotArgs& a, int size) {
+  const int lane = threadIdx.x & 63;
+  int64_t all = 0;
+  for (int64_t e0 = 0; e0 < a.experts; e0 += 64) {
+    const int64_t e = e0 + lane;
+    int64_t lo = 0, hi = 0;
+    if (e < a.experts) f8_rows_of(a, e, &lo, &hi);
+    all += __builtin_amdgcn_readlane(lanes_up_to(int32_t((hi - lo + size - 1) / size), lane), 63);
+  }
+  return all;
+}
+
+// The tile-th of those tiles; every wave finds it by itself.
+__device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile, int size) {
   const int lane = threadIdx.x & 63;
   int64_t before = 0;
   for (int64_t e0 = 0; e0 < a.experts; e0 += 64) {
@@ -43,20 +55,17 @@ __device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile
     const uint64_t behind = __ballot(before + upto > tile);
     if (behind) {
       const int first = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)behind) - 1);
-      F8Rows r;
       const int64_t row = lo + (tile - before - (upto - tiles)) * size;
-      const int32_t row32 = __builtin_amdgcn_readlane(int32_t(row), first), lo32 = __builtin_amdgcn_readlane(int32_t(lo), first),
-                    hi32 = __builtin_amdgcn_readlane(int32_t(hi), first);
-      r.first = row32;
-      r.end = hi32;
+      F8Rows r;
+      r.first = __builtin_amdgcn_readlane(int32_t(row), first);
+      r.end = __builtin_amdgcn_readlane(int32_t(hi), first);
       // (offsets that go down could give a number of tiles that has overflowed)
-      if (row32 < lo32) r.end = r.first;
+      if (r.first < __builtin_amdgcn_readlane(int32_t(lo), first)) r.end = r.first;
       r.expert = e0 + first;
       return r;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
-  *all = before;
   return F8Rows{0, 0, 0};
 }
 
