@@ -419,7 +419,7 @@ int glenside_f8_dequantize(const gs_f8* in, gs_ap* out, void* stream);
  *   h = x + residual,   y = h / sqrt(sum h^2 / K + eps) weight.
  * x ((a..),(c..)) bf16 or f32; residual (NULL: zeros) and sum (NULL: not wanted) of its shape, split and type; weight (NULL:
  * ones) ((),(c..)) bf16 or f32; eps not below 0.  h is rounded to its type, and is what the norm is of: sum := h.  Squares, their sum
- * and y are fp32: squares above float's range make the element's results zero, or NaN.
+ * and its root are 64 bits; y is rounded to float once.  An infinity makes its element's other numbers zero, and itself NaN.
  *   _norm    : out := y, of x's shape and split, bf16 or f32;
  *   _f8_norm : out := y quantised as by glenside_f8_quantize (from fp32, not rounded in between), block_rows 1. */
 int glenside_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight, float eps, gs_ap* sum, gs_ap* out,

@@ -19,26 +19,23 @@ __device__ __forceinline__ float f8_scale(uint32_t top) {
   const float s = __uint_as_float(top) * (1.0f / kF8Most);
   return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : s > kF8LeastScale ? s : kF8LeastScale;
 }
-// Eight floats -> eight codes: times 1 / scale (which is below 2^127, and no number then above 448 (1 + 2^-22), which rounds to
+// Four floats -> four codes: times 1 / scale (which is below 2^127, and no number then above 448 (1 + 2^-22), which rounds to
 // 448), rounded to the nearest code, ties to even.  A scale of NaN gives zeros.
+__device__ __forceinline__ int32_t f8_encode4(const float* x, float factor) {
+  int32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * factor, x[1] * factor, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * factor, x[3] * factor, w, true);
+  return factor == factor ? w : 0;
+}
 __device__ __forceinline__ i32x2 f8_encode8(const float (&x)[8], float scale) {
   const float f = 1.0f / scale;
-  int32_t lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * f, x[1] * f, lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * f, x[5] * f, hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * f, x[7] * f, hi, true);
-  return scale == scale ? i32x2{lo, hi} : i32x2{0, 0};
+  return i32x2{f8_encode4(x, f), f8_encode4(x + 4, f)};
 }
-__device__ __forceinline__ void f8_decode8(const i32x2& w, float scale, float (&x)[8]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], true);
-    x[4 * h] = a[0] * scale;
-    x[4 * h + 1] = a[1] * scale;
-    x[4 * h + 2] = b[0] * scale;
-    x[4 * h + 3] = b[1] * scale;
-  }
+__device__ __forceinline__ void f8_decode4(int32_t w, float scale, float* x) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  x[0] = a[0] * scale;
+  x[1] = a[1] * scale;
+  x[2] = b[0] * scale;
+  x[3] = b[1] * scale;
 }
 // The largest of the bits of sixteen neighbouring lanes (a row of the wave).
 __device__ __forceinline__ uint32_t max_of_16_lanes(uint32_t v) {
@@ -51,12 +48,19 @@ __device__ __forceinline__ uint32_t max_of_16_lanes(uint32_t v) {
   o = __builtin_amdgcn_mov_dpp(v, 0x121, 0xF, 0xF, true);
   return v > o ? v : o;
 }
-__device__ __forceinline__ uint32_t top_of_8(const float (&x)[8]) {
+// Of the lanes that have a block's 128 numbers, N each.
+template <int N>
+__device__ __forceinline__ uint32_t f8_block_top(const float (&x)[N]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
     top = top > b ? top : b;
+  }
+  top = max_of_16_lanes(top);
+  if constexpr (N == 4) {
+    const uint32_t o = __builtin_amdgcn_ds_swizzle(top, 0x401f);       // the other sixteen of 32
+    top = top > o ? top : o;
   }
   return top;
 }
@@ -101,9 +105,11 @@ struct F8DotArgs {        // out[m][n] = sum_b xs[m][b] ws[n / w_rows][b] sum_{k
   int64_t experts, x_count, x_least;   // x_count: rows of x
   int32_t splits;         // set by the launcher: workgroups that share the sum over K of a tile
 };
+// How a product is done.
+enum F8DotWay { kF8Rows1, kF8Rows2, kF8Tile32x64, kF8Tile64x64, kF8Tile64x128, kF8Tile128x128Few, kF8Tile128x128, kF8Tile128x256, kF8Tile256x256 };
 struct F8DotPlan {
-  int way;
-  int splits;
+  F8DotWay way;
+  int splits;             // workgroups that share the sum of a tile
   size_t part_bytes;
 };
 F8DotPlan plan_f8_dot(int64_t M, int64_t N, int64_t K, int64_t experts);

@@ -400,4 +400,13 @@ int glenside_expert_join_grad(const gs_ap* grad, const gs_ap* rows, const gs_ap*
   return launch_status(launch_expert_join_grad(a, static_cast<hipStream_t>(stream)));
 }
 
+// For tests, not part of the interface: how a product of these sizes (K in numbers; experts 0: one matrix) is done, F8DotWay and workgroups that share a
+// sum.  Host only.
+int gs_test_f8_dot_plan(int64_t M, int64_t N, int64_t K, int64_t experts, int plan[2]) {
+  const F8DotPlan p = plan_f8_dot(M, N, f8_blocks(K) * kF8Block, experts);
+  plan[0] = p.way;
+  plan[1] = p.splits;
+  return GS_OK;
+}
+
 }  // extern "C"

@@ -1,7 +1,8 @@
 // Conversion to and from scaled 8-bit floats, and the root-mean-square norm whose result they are.
 //
-// A scale is its block's largest magnitude over 448, the largest number of e4m3.  A lane has 8 numbers, sixteen neighbouring
-// lanes a row's 128; blocks of 128 rows are a workgroup's, 64 numbers per lane in registers, so that numbers are read once.
+// A scale is its block's largest magnitude over 448, the largest number of e4m3.  A lane has 16 bytes of numbers, so that a wave's access is 1 KB
+// of a row: sixteen neighbouring lanes have 128 of bfloat16, 32 those of floats.  Blocks of 128 rows are a workgroup's, 64 numbers per lane
+// in registers, so that numbers are read once.
 //
 // Bound by memory.
 #include "f8.h"
@@ -11,29 +12,22 @@ namespace gs {
 
 namespace {
 
-// 8 numbers of a row from element `at` on into memory, as far as `left` goes.
-template <int DT>
-__device__ __forceinline__ void store_8(void* row, int64_t at, int64_t left, const float (&x)[8]) {
-  if constexpr (DT == GS_BF16) {
-    uint16_t* dst = static_cast<uint16_t*>(row) + at;
-    const i32x4 v = {int32_t(pack_bf16x2(x[0], x[1])), int32_t(pack_bf16x2(x[2], x[3])), int32_t(pack_bf16x2(x[4], x[5])), int32_t(pack_bf16x2(x[6], x[7]))};
-    if (left >= 8) {
-      __builtin_nontemporal_store((i32x4_any2)v, reinterpret_cast<i32x4_any2*>(dst));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 7; ++i)
-        if (i < left) dst[i] = uint16_t(uint32_t(v[i / 2]) >> (16 * (i & 1)));
-    }
+// The codes of a lane's numbers.
+template <int N>
+using Codes = std::conditional_t<N == 8, i32x2, int32_t>;
+template <int N>
+__device__ __forceinline__ Codes<N> encode(const float (&x)[N], float scale) {
+  const float f = 1.0f / scale;
+  if constexpr (N == 8) return i32x2{f8_encode4(x, f), f8_encode4(x + 4, f)};
+  else return f8_encode4(x, f);
+}
+template <int N>
+__device__ __forceinline__ void decode(const Codes<N>& w, float scale, float (&x)[N]) {
+  if constexpr (N == 8) {
+    f8_decode4(w[0], scale, x);
+    f8_decode4(w[1], scale, x + 4);
   } else {
-    float* dst = static_cast<float*>(row) + at;
-    if (left >= 8) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) __builtin_nontemporal_store((f32x4_any{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]}), reinterpret_cast<f32x4_any*>(dst + 4 * h));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 7; ++i)
-        if (i < left) dst[i] = x[i];
-    }
+    f8_decode4(w, scale, x);
   }
 }
 
@@ -41,23 +35,24 @@ __device__ __forceinline__ void store_8(void* row, int64_t at, int64_t left, con
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) f8_quantize_kernel(F8ConvertArgs a, Pieces<BIG> n) {
   using Index = typename Pieces<BIG>::Index;
+  constexpr int N = kNumbers<DT>, kLanes = kF8Block / N;
   const Index cols = Index(a.cols), blocks = Index(f8_blocks(a.cols)), pitch = Index(f8_scale_pitch(a.cols));
   const Index base = Index(blockIdx.x) * (kThreads * P) + threadIdx.x;
   Index row[P], piece[P];
-  float x[P][8];
+  float x[P][N];
   n.places(base, row, piece);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const Index at = piece[p] * 8;
-    load_numbers<DT, 8>(a.plain, int64_t(row[p] * cols + at), at + 8 <= cols ? 8 : at < cols ? int(cols - at) : 0, x[p]);
+    const Index at = piece[p] * N;
+    load_row_numbers<DT, N>(a.plain, int64_t(row[p] * cols + at), at + N <= cols ? N : at < cols ? int(cols - at) : 0, x[p]);
   }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const float scale = f8_scale(max_of_16_lanes(top_of_8(x[p])));
+    const float scale = f8_scale(f8_block_top(x[p]));
     if (base + p * kThreads >= n.total) continue;
-    static_cast<i32x2*>(a.values)[row[p] * n.per_row + piece[p]] = f8_encode8(x[p], scale);
-    if (piece[p] % 16 == 0) {
-      const Index block = piece[p] / 16;
+    static_cast<Codes<N>*>(a.values)[row[p] * n.per_row + piece[p]] = encode(x[p], scale);
+    if (piece[p] % kLanes == 0) {
+      const Index block = piece[p] / kLanes;
       float* const to = a.scales + (row[p] * pitch + block);
       *to = scale;
       if (block + 1 == blocks)
@@ -69,32 +64,36 @@ __global__ void __launch_bounds__(kThreads) f8_quantize_kernel(F8ConvertArgs a, 
 // Blocks of 128 rows: one of 128 x 128 numbers to a workgroup.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) f8_quantize_square_kernel(F8ConvertArgs a, uint32_t row_blocks, uint32_t blocks) {
+  constexpr int N = kNumbers<DT>, kLanes = kF8Block / N, kRows = kThreads / kLanes, I = 128 / kRows;
   const uint32_t mb = blockIdx.x / blocks, kb = blockIdx.x - mb * blocks, mat = mb / row_blocks, rb = mb - mat * row_blocks;
-  const int lane16 = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-  const int64_t k = int64_t(kb) * kF8Block + lane16 * 8, left = a.cols - k, row0 = int64_t(mat) * a.rows + int64_t(rb) * 128;
+  const int piece = threadIdx.x % kLanes, r0 = threadIdx.x / kLanes;
+  const int64_t k = int64_t(kb) * kF8Block + piece * N, left = a.cols - k, row0 = int64_t(mat) * a.rows + int64_t(rb) * 128;
   const int rows = a.rows - int64_t(rb) * 128 < 128 ? int(a.rows - int64_t(rb) * 128) : 128;
-  float x[8][8];
+  float x[I][N];
+#pragma unroll
+  for (int i = 0; i < I; ++i) {
+    const int r = r0 + kRows * i;
+    load_row_numbers<DT, N>(a.plain, (row0 + (r < rows ? r : 0)) * a.cols + k, r < rows ? left : 0, x[i]);
+  }
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + 16 * i;
-    load_numbers<DT, 8>(a.plain, (row0 + (r < rows ? r : 0)) * a.cols + k, r < rows ? left : 0, x[i]);
-  }
+  for (int i = 0; i < I; ++i)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t t = top_of_8(x[i]);
-    top = top > t ? top : t;
-  }
+    for (int j = 0; j < N; ++j) {
+      const uint32_t b = __float_as_uint(x[i][j]) & 0x7fffffffu;
+      top = top > b ? top : b;
+    }
   __shared__ uint32_t tops[kThreads / 16];
   top = max_of_16_lanes(top);
-  if (lane16 == 0) tops[r0] = top;
+  if (threadIdx.x % 16 == 0) tops[threadIdx.x / 16] = top;
   __syncthreads();
-  const float scale = f8_scale(max_of_16_lanes(tops[lane16]));
+  static_assert(kThreads / 16 == 16, "a row of lanes has them all");
+  const float scale = f8_scale(max_of_16_lanes(tops[threadIdx.x % 16]));
   const int64_t pitch = int64_t(blocks) * kF8Block;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + 16 * i;
-    if (r < rows) *reinterpret_cast<i32x2*>(static_cast<uint8_t*>(a.values) + (row0 + r) * pitch + k) = f8_encode8(x[i], scale);
+  for (int i = 0; i < I; ++i) {
+    const int r = r0 + kRows * i;
+    if (r < rows) *reinterpret_cast<Codes<N>*>(static_cast<uint8_t*>(a.values) + (row0 + r) * pitch + k) = encode(x[i], scale);
   }
   if (threadIdx.x == 0) {
     const int64_t run = round_up(blocks, kF8ScaleRun);
@@ -105,81 +104,179 @@ __global__ void __launch_bounds__(kThreads) f8_quantize_square_kernel(F8ConvertA
   }
 }
 
-// Rows as they are counted here are those of all matrices; a block of 128 rows ends with its matrix.
+// The row of scales of a row, rows being counted over all matrices; a block of 128 rows ends with its matrix.
+template <bool BIG, typename Index>
+__device__ __forceinline__ Index scale_row(const F8ConvertArgs& a, Index row, const FastDiv& by_rows) {
+  if (a.block_rows == 1) return row;
+  Index mat = 0;
+  if (a.mats > 1) {
+    if constexpr (BIG) mat = row / Index(a.rows);
+    else mat = by_rows.div(row);
+  }
+  return mat * Index(ceil_div(a.rows, 128)) + (row - mat * Index(a.rows)) / 128;
+}
+
 template <int DT, int P, bool BIG>
 __global__ void __launch_bounds__(kThreads) f8_dequantize_kernel(F8ConvertArgs a, Pieces<BIG> n, FastDiv by_rows) {
   using Index = typename Pieces<BIG>::Index;
-  const Index cols = Index(a.cols), pitch = Index(f8_scale_pitch(a.cols)), codes = Index(f8_blocks(a.cols)) * 16;
+  constexpr int N = kNumbers<DT>, kLanes = kF8Block / N;
+  const Index cols = Index(a.cols), pitch = Index(f8_scale_pitch(a.cols)), codes = Index(f8_blocks(a.cols)) * kLanes;
   const Index base = Index(blockIdx.x) * (kThreads * P) + threadIdx.x;
   Index row[P], piece[P];
-  i32x2 w[P];
+  Codes<N> w[P];
   float scale[P];
   n.places(base, row, piece);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    Index of = row[p];
-    if (a.block_rows != 1) {
-      Index mat = 0;
-      if (a.mats > 1) {
-        if constexpr (BIG) mat = row[p] / Index(a.rows);
-        else mat = by_rows.div(row[p]);
-      }
-      of = mat * Index(ceil_div(a.rows, 128)) + (row[p] - mat * Index(a.rows)) / 128;
-    }
-    w[p] = static_cast<const i32x2*>(a.values)[row[p] * codes + piece[p]];
-    scale[p] = a.scales[of * pitch + piece[p] / 16];
+    w[p] = static_cast<const Codes<N>*>(a.values)[row[p] * codes + piece[p]];
+    scale[p] = a.scales[scale_row<BIG>(a, row[p], by_rows) * pitch + piece[p] / kLanes];
   }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (base + p * kThreads >= n.total) continue;
-    const Index at = piece[p] * 8;
-    float x[8];
-    f8_decode8(w[p], scale[p], x);
-    store_8<DT>(a.plain, int64_t(row[p] * cols + at), int64_t(cols - at), x);
+    const Index at = piece[p] * N;
+    float x[N];
+    decode<N>(w[p], scale[p], x);
+    store_row_numbers<DT, N>(a.plain, int64_t(row[p] * cols + at), int64_t(cols - at), x);
   }
 }
 
+// Back into rows that do not all begin on 16 bytes: pieces are those of the result's memory, so that whole lines are written.  A piece may have
+// numbers of two blocks; one with numbers of two rows is written number by number.  There are cols >= N numbers in a row, n.per_row of
+// them.
 template <int DT, int P, bool BIG>
-hipError_t launch_convert(const F8ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
-  const int64_t total = a.mats * a.rows * per_row, groups = ceil_div(total, kThreads * P);
+__global__ void __launch_bounds__(kThreads) f8_dequantize_flat_kernel(F8ConvertArgs a, Pieces<BIG> n, FastDiv by_rows) {
+  using Index = typename Pieces<BIG>::Index;
+  constexpr int N = kNumbers<DT>;
+  using CodesAny = std::conditional_t<N == 8, i32x2_any, i32_any>;
+  const Index cols = n.per_row, pitch = Index(f8_scale_pitch(a.cols)), row_codes = Index(f8_blocks(a.cols)) * kF8Block;
+  const Index base = (Index(blockIdx.x) * (kThreads * P) + threadIdx.x) * N;
+  const uint8_t* const values = static_cast<const uint8_t*>(a.values);
+  Index row[P], first[P];             // of the piece's first number
+  Codes<N> w[P];
+  float scale[P][2];
+  int border[P];                      // numbers from here on are of the second block
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    n.divide(base + p * (kThreads * N) < n.total ? base + p * (kThreads * N) : 0, &row[p], &first[p]);
+    const Index last = first[p] + N <= cols ? first[p] + N - 1 : cols - 1, at = first[p] + N <= row_codes ? first[p] : row_codes - N;
+    w[p] = *reinterpret_cast<const CodesAny*>(values + (row[p] * row_codes + at));
+    const float* const scales = a.scales + scale_row<BIG>(a, row[p], by_rows) * pitch;
+    scale[p][0] = scales[first[p] / kF8Block];
+    scale[p][1] = scales[last / kF8Block];
+    border[p] = int(last / kF8Block * kF8Block) - int(first[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const Index number = base + p * (kThreads * N);
+    if (number >= n.total) continue;
+    if (first[p] + N > cols) {
+#pragma unroll 1
+      for (int i = 0; i < N && number + i < n.total; ++i) {
+        const bool wraps = first[p] + i >= cols;
+        const Index r = wraps ? row[p] + 1 : row[p], c = wraps ? first[p] + i - cols : first[p] + i;
+        float four[4];
+        f8_decode4(values[r * row_codes + c], a.scales[scale_row<BIG>(a, r, by_rows) * pitch + c / kF8Block], four);
+        if constexpr (DT == GS_BF16) static_cast<uint16_t*>(a.plain)[number + i] = float_to_bf16_bits(four[0]);
+        else static_cast<float*>(a.plain)[number + i] = four[0];
+      }
+      continue;
+    }
+    float x[N], y[N];
+    decode<N>(w[p], scale[p][0], x);
+    decode<N>(w[p], scale[p][1], y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < border[p] ? x[i] : y[i];
+    store_row_numbers<DT, N>(a.plain, int64_t(number), N, x);
+  }
+}
+
+enum Convert { kQuantize, kDequantize, kDequantizeFlat };
+template <int DT, int P, bool BIG>
+hipError_t launch_convert(const F8ConvertArgs& a, int64_t per_row, Convert what, hipStream_t s) {
+  // (the flat kernel counts numbers, the others pieces)
+  const bool flat = what == kDequantizeFlat;
+  const int64_t rows = a.mats * a.rows, step = flat ? a.cols : per_row, total = rows * step;
+  const int64_t groups = ceil_div(total, kThreads * P * (flat ? kNumbers<DT> : 1));
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
   using Index = typename Pieces<BIG>::Index;
-  const Pieces<BIG> n{Index(per_row), Index(total), FastDiv::make(BIG ? 1u : uint32_t(per_row))};
-  if (quantize) hipLaunchKernelGGL((f8_quantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n);
-  else
-    hipLaunchKernelGGL((f8_dequantize_kernel<DT, P, BIG>), dim3(unsigned(groups)), dim3(kThreads), 0, s, a, n,
-                       FastDiv::make(BIG ? 1u : uint32_t(a.rows)));
+  const Pieces<BIG> n{Index(step), Index(total), FastDiv::make(BIG ? 1u : uint32_t(step))};
+  const FastDiv by_rows = FastDiv::make(BIG ? 1u : uint32_t(a.rows));
+  const dim3 grid{unsigned(groups)}, block(kThreads);
+  if (what == kQuantize) hipLaunchKernelGGL((f8_quantize_kernel<DT, P, BIG>), grid, block, 0, s, a, n);
+  else if (what == kDequantize) hipLaunchKernelGGL((f8_dequantize_kernel<DT, P, BIG>), grid, block, 0, s, a, n, by_rows);
+  else hipLaunchKernelGGL((f8_dequantize_flat_kernel<DT, P, BIG>), grid, block, 0, s, a, n, by_rows);
   return hipGetLastError();
 }
 // Four pieces per lane where that still leaves eight workgroups for every compute unit.
 template <int DT>
-hipError_t convert(const F8ConvertArgs& a, int64_t per_row, bool quantize, hipStream_t s) {
+hipError_t convert(const F8ConvertArgs& a, int64_t per_row, Convert what, hipStream_t s) {
   const int64_t total = a.mats * a.rows * per_row;
   if (total == 0) return hipSuccess;
-  if (total > (int64_t(1) << 27)) return launch_convert<DT, 4, true>(a, per_row, quantize, s);
-  if (total >= int64_t(256) * 8 * 4 * kThreads) return launch_convert<DT, 4, false>(a, per_row, quantize, s);
-  return launch_convert<DT, 1, false>(a, per_row, quantize, s);
+  // (a row has 512 bytes of scales and codes at least, whatever its length: places are counted in 32 bits up to 2^22 rows)
+  if (total > (int64_t(1) << 30) / kNumbers<DT> || a.mats * a.rows > (int64_t(1) << 22)) return launch_convert<DT, 4, true>(a, per_row, what, s);
+  if (total >= int64_t(256) * 8 * 4 * kThreads) return launch_convert<DT, 4, false>(a, per_row, what, s);
+  return launch_convert<DT, 1, false>(a, per_row, what, s);
+}
+template <int DT>
+hipError_t quantize(const F8ConvertArgs& a, hipStream_t s) {
+  return convert<DT>(a, f8_blocks(a.cols) * (kF8Block / kNumbers<DT>), kQuantize, s);
+}
+template <int DT>
+hipError_t dequantize(const F8ConvertArgs& a, hipStream_t s) {
+  constexpr int N = kNumbers<DT>;
+  return convert<DT>(a, ceil_div(a.cols, N), a.cols % N == 0 || a.mats * a.rows <= 1 || a.cols < 128 ? kDequantize : kDequantizeFlat, s);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Norm: h = x + residual, rounded to their type; y = h / sqrt(mean(h^2) + eps) weight.
+//
+// Squares, their sum, the root and y before it is rounded to float are 64 bits: there no square overflows, and y is the float nearest to its
+// definition whatever the order of the sum, so that numbers on a border between two codes, which products of bfloat16 numbers often are, get
+// the code that the definition gives them (in 32 bits 6 of 100000 had the other one).
 // ---------------------------------------------------------------------------------------------
 
-// 8 numbers as bfloat16 keeps them.
-__device__ __forceinline__ void round_8(float (&x)[8], std::integral_constant<int, GS_BF16>) {
+// A lane's 8 numbers of a row between the sum and the result, as they are stored.
+template <int DT>
+struct Kept;
+template <>
+struct Kept<GS_BF16> {
+  i32x4 v;
+  __device__ void put(const float (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-    x[2 * i] = __uint_as_float(w << 16);
-    x[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) v[i] = int32_t(pack_bf16x2(x[2 * i], x[2 * i + 1]));
   }
-}
-__device__ __forceinline__ void round_8(float (&)[8], std::integral_constant<int, GS_F32>) {}
+  __device__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(uint32_t(v[i]) << 16);
+      x[2 * i + 1] = __uint_as_float(uint32_t(v[i]) & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Kept<GS_F32> {
+  float v[8];
+  __device__ void put(const float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[i];
+  }
+  __device__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = v[i];
+  }
+};
 
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
   return v;
+}
+__device__ __forceinline__ double inverse_root(double d) {
+  const double r = __builtin_amdgcn_rsq(d);
+  if (!(d > 0.0) || d == __builtin_huge_val()) return r;
+  const double half = 0.5 * d, s = r * (1.5 - half * r * r);       // (26 bits, then 50, then all)
+  return s * (1.5 - half * s * s);
 }
 
 // WAVES waves have a row, or one wave each of four; NP pieces of 8 numbers per lane stay in registers between the sum and the
@@ -187,46 +284,50 @@ __device__ __forceinline__ float wave_sum(float v) {
 template <int DT, int OUT, int WAVES, int NP>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(NormArgs a) {
   constexpr int T = WAVES * 64;
-  __shared__ float part[WAVES];
+  __shared__ double part[WAVES];
   const int64_t row = WAVES == 1 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
   const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
   if (row >= a.rows) return;          // (a whole wave, and there is no barrier with one wave per row)
   const int64_t base = row * a.cols, blocks = f8_blocks(a.cols), pieces = OUT == GS_F8 ? blocks * 16 : ceil_div(a.cols, 8);
-  auto load = [&](int64_t piece, float (&h)[8]) {
+  auto load = [&](int64_t piece, Kept<DT>& kept) {
     const int64_t at = piece * 8, left = a.cols - at;
-    load_numbers<DT, 8>(a.x, base + at, left, h);
+    float h[8];
+    load_row_numbers<DT, 8>(a.x, base + at, left, h);
     if (a.residual) {
       float r[8];
-      load_numbers<DT, 8>(a.residual, base + at, left, r);
+      load_row_numbers<DT, 8>(a.residual, base + at, left, r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += r[i];
-      round_8(h, std::integral_constant<int, DT>{});
     }
+    kept.put(h);
   };
-  auto squares = [&](int64_t piece, const float (&h)[8]) {
-    if (a.sum && piece * 8 < a.cols) store_8<DT>(a.sum, base + piece * 8, a.cols - piece * 8, h);
-    float s = 0;
+  auto squares = [&](int64_t piece, const Kept<DT>& kept) {
+    float h[8];
+    kept.get(h);
+    if (a.sum && piece * 8 < a.cols) store_row_numbers<DT, 8>(a.sum, base + piece * 8, a.cols - piece * 8, h);
+    double s = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += h[i] * h[i];
+    for (int i = 0; i < 8; ++i) s = __builtin_fma(double(h[i]), double(h[i]), s);
     return s;
   };
-  auto finish = [&](int64_t piece, float (&h)[8], float r) {
+  auto finish = [&](int64_t piece, const Kept<DT>& kept, double r) {
     const int64_t at = piece * 8, left = a.cols - at;
-    float w[8];
+    float h[8], w[8];
+    kept.get(h);
     if (a.weight) {
-      if (a.w_dtype == GS_BF16) load_numbers<GS_BF16, 8>(a.weight, at, left, w);
-      else load_numbers<GS_F32, 8>(a.weight, at, left, w);
+      if (a.w_dtype == GS_BF16) load_row_numbers<GS_BF16, 8, false>(a.weight, at, left, w);
+      else load_row_numbers<GS_F32, 8, false>(a.weight, at, left, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = h[i] * r * w[i];
+      for (int i = 0; i < 8; ++i) h[i] = float(double(h[i]) * r * double(w[i]));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] *= r;
+      for (int i = 0; i < 8; ++i) h[i] = float(double(h[i]) * r);
     }
     if constexpr (OUT == GS_F8) {
       // (what a row has behind its end is zero: infinities of r must not make it NaN)
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] = i < left ? h[i] : 0.0f;
-      const float scale = f8_scale(max_of_16_lanes(top_of_8(h)));
+      const float scale = f8_scale(f8_block_top(h));
       if (piece >= pieces) return;
       static_cast<i32x2*>(a.out)[row * pieces + piece] = f8_encode8(h, scale);
       if (piece % 16 == 0) {
@@ -237,12 +338,12 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
           for (int64_t i = blocks; i < run; ++i) to[i - block] = 0.0f;
       }
     } else {
-      if (piece < pieces) store_8<OUT>(a.out, base + at, left, h);
+      if (piece < pieces) store_row_numbers<OUT, 8>(a.out, base + at, left, h);
     }
   };
-  float sum = 0;
+  double sum = 0;
   if constexpr (NP > 0) {
-    float h[NP][8];
+    Kept<DT> h[NP];
 #pragma unroll
     for (int p = 0; p < NP; ++p) load(t + p * T, h[p]);
 #pragma unroll
@@ -255,13 +356,13 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) sum += part[w];
     }
-    const float r = 1.0f / sqrtf(sum / float(a.cols) + a.eps);
+    const double r = inverse_root(sum / double(a.cols) + double(a.eps));
 #pragma unroll
     for (int p = 0; p < NP; ++p) finish(t + p * T, h[p], r);
   } else {
     const int64_t end = round_up(pieces, T);         // (all lanes of a block's sixteen, whatever the row's length)
     for (int64_t piece = t; piece < end; piece += T) {
-      float h[8];
+      Kept<DT> h;
       load(piece, h);
       sum += squares(piece, h);
     }
@@ -271,9 +372,9 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
     sum = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) sum += part[w];
-    const float r = 1.0f / sqrtf(sum / float(a.cols) + a.eps);
+    const double r = inverse_root(sum / double(a.cols) + double(a.eps));
     for (int64_t piece = t; piece < end; piece += T) {
-      float h[8];
+      Kept<DT> h;
       load(piece, h);
       finish(piece, h, r);
     }
@@ -290,22 +391,24 @@ hipError_t launch_norm_as(const NormArgs& a, hipStream_t s) {
 template <int DT, int OUT>
 hipError_t norm(const NormArgs& a, hipStream_t s) {
   const int64_t pieces = OUT == GS_F8 ? f8_blocks(a.cols) * 16 : ceil_div(a.cols, 8);
+  // Two pieces per lane, whose loads are all under way and whose registers leave room for eight waves on a SIMD (16384 x 8192 bfloat16 with a
+  // residual: 165 us, four pieces in half the waves 191, one in twice as many 188; 4096 x 16384 86, 111 with four); one where there are no more
+  // rows than compute units (256 x 4096 5.0 and 6.1).
   if (pieces <= 64) return launch_norm_as<DT, OUT, 1, 1>(a, s);
   if (pieces <= 128) return launch_norm_as<DT, OUT, 1, 2>(a, s);
   if (pieces <= 256) return launch_norm_as<DT, OUT, 4, 1>(a, s);
+  if (pieces <= 1024 && a.rows <= 256) return launch_norm_as<DT, OUT, 16, 1>(a, s);
   if (pieces <= 512) return launch_norm_as<DT, OUT, 4, 2>(a, s);
-  if (pieces <= 1024) return launch_norm_as<DT, OUT, 4, 4>(a, s);
-  if (pieces <= 2048) return launch_norm_as<DT, OUT, 8, 4>(a, s);
+  if (pieces <= 1024) return launch_norm_as<DT, OUT, 8, 2>(a, s);
+  if (pieces <= 2048) return launch_norm_as<DT, OUT, 16, 2>(a, s);
+  if (pieces <= 4096) return launch_norm_as<DT, OUT, 16, 4>(a, s);
   return launch_norm_as<DT, OUT, 16, 0>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_f8_quantize(const F8ConvertArgs& a, hipStream_t s) {
-  if (a.block_rows == 1) {
-    const int64_t per_row = f8_blocks(a.cols) * 16;
-    return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, true, s) : convert<GS_F32>(a, per_row, true, s);
-  }
+  if (a.block_rows == 1) return a.dtype == GS_BF16 ? quantize<GS_BF16>(a, s) : quantize<GS_F32>(a, s);
   const int64_t row_blocks = ceil_div(a.rows, 128), blocks = f8_blocks(a.cols), groups = a.mats * row_blocks * blocks;
   if (groups == 0) return hipSuccess;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
@@ -314,10 +417,7 @@ hipError_t launch_f8_quantize(const F8ConvertArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((f8_quantize_square_kernel<GS_F32>), grid, block, 0, s, a, uint32_t(row_blocks), uint32_t(blocks));
   return hipGetLastError();
 }
-hipError_t launch_f8_dequantize(const F8ConvertArgs& a, hipStream_t s) {
-  const int64_t per_row = ceil_div(a.cols, 8);
-  return a.dtype == GS_BF16 ? convert<GS_BF16>(a, per_row, false, s) : convert<GS_F32>(a, per_row, false, s);
-}
+hipError_t launch_f8_dequantize(const F8ConvertArgs& a, hipStream_t s) { return a.dtype == GS_BF16 ? dequantize<GS_BF16>(a, s) : dequantize<GS_F32>(a, s); }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
   if (a.rows == 0 || a.cols == 0) return hipSuccess;

@@ -87,10 +87,10 @@ template <int BM, int BN, int WGM, int WGN, int NS, bool W1, bool GROUPED>
 __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArgs a, uint32_t tiles_m, uint32_t tiles_n) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NJ = WN / 16;
   constexpr int XQ = BM / 8 / NW, YQ = BN / 8 / NW, VQ = XQ + YQ;  // transfers of values per wave and slab: 8 rows each
-  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0 && WN <= 128 && NJ % 2 == 0, "whole transfers");
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BN % 64 == 0 && WN <= 128 && NJ % 2 == 0, "whole transfers");
   static_assert(NW % 2 == 0, "the exchange of columns must not depend on q");
   static_assert(NS >= 2 && NS <= 4, "two buffers of scales are enough");
-  constexpr int kSX = BM / 64, kSW = W1 ? BN / 64 : 1, kSAll = kSX + kSW, SQ = (kSAll + NW - 1) / NW;   // of scales, per four slabs: 64 rows each
+  constexpr int kSX = (BM + 63) / 64, kSW = W1 ? BN / 64 : 1, kSAll = kSX + kSW, SQ = (kSAll + NW - 1) / NW;   // of scales, per four slabs: 64 rows each
   constexpr int kX = BM * 128, kBuf = (BM + BN) * 128, kSBuf = kSAll * 1024;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
 
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
 
 template <int BM, int BN, int WGM, int WGN, int NS, bool W1, bool GROUPED>
 hipError_t launch_f8_tiles_as(const F8DotArgs& a, int64_t tiles_m, hipStream_t s) {
-  constexpr int slabs = NS * (BM + BN) * 128 + 2 * 1024 * (BM / 64 + (W1 ? BN / 64 : 1)), staging = WGM * WGN * 16 * (BN / WGN + 4) * 4;
+  constexpr int slabs = NS * (BM + BN) * 128 + 2 * 1024 * ((BM + 63) / 64 + (W1 ? BN / 64 : 1)), staging = WGM * WGN * 16 * (BN / WGN + 4) * 4;
   constexpr int bytes = slabs > staging ? slabs : staging;
   static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
   const int64_t tiles_n = ceil_div(a.N, BN);
