@@ -168,8 +168,9 @@ int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * c
 // Tiles: what a launch of them takes to begin, a slab where a compute unit has one workgroup, and where several share it or follow each
 // other on it, and what each of those that follow takes more (us).  All of them are bound by the transfers to LDS, 50 to 70 bytes per
 // nanosecond and compute unit (80 where all slabs are in L2: the same kernels without products and fragments), until the largest tiles'
-// products take as long: 8192 cubed 460 us, 386 without transfers behind the first slabs, 334 with nothing else.  (Lines requested into L2 by
-// one workgroup of those that share them, two to eight slabs ahead: 472.)
+// products take as long: 8192 cubed 460 us before transfers were spread over columns (439), 386 without transfers behind the first slabs, 334 with nothing
+// else.  (Lines requested into L2 by one workgroup of those that share them, two to eight slabs ahead: 472; six or eight slabs under way in place of four:
+// 333 x 5000 x 4104 18.5 us, 18.0 with four in 64x128 tiles of four waves, 16.5 of eight.)
 struct TileWay {
   F8DotWay way;
   int bm, bn;
@@ -178,7 +179,7 @@ struct TileWay {
 constexpr TileWay kTileWays[] = {{kF8Tile32x64, 32, 64, 1.5, 0.29, 0.205, 0.0},    {kF8Tile64x64, 64, 64, 1.5, 0.35, 0.27, 0.0},
                                  {kF8Tile64x128, 64, 128, 2.0, 0.47, 0.47, 0.0},   {kF8Tile128x128Few, 128, 128, 2.5, 0.64, 0.64, 2.0},
                                  {kF8Tile128x128, 128, 128, 2.5, 0.9, 0.57, 0.0},  {kF8Tile128x256, 128, 256, 3.0, 0.9, 1.03, 3.0},
-                                 {kF8Tile256x256, 256, 256, 4.0, 1.5, 1.77, 4.0}};
+                                 {kF8Tile256x256, 256, 256, 4.0, 1.35, 1.72, 4.0}};
 
 }  // namespace
 
@@ -243,11 +244,11 @@ hipError_t launch_f8_dot(const F8DotArgs& given, const F8DotPlan& plan, void* wo
     case kF8Rows2: e = launch_rows<2>(b, s); break;
     case kF8Tile32x64: e = launch_f8_tiles<32, 64, 2, 2, 4>(b, most_tiles(a, 32), s); break;
     case kF8Tile64x64: e = launch_f8_tiles<64, 64, 2, 2, 4>(b, most_tiles(a, 64), s); break;
-    case kF8Tile64x128: e = launch_f8_tiles<64, 128, 2, 2, 4>(b, most_tiles(a, 64), s); break;
-    case kF8Tile128x128Few: e = launch_f8_tiles<128, 128, 2, 4, 4>(b, most_tiles(a, 128), s); break;
+    case kF8Tile64x128: e = launch_f8_tiles<64, 128, 2, 4, 4>(b, most_tiles(a, 64), s); break;
+    case kF8Tile128x128Few: e = launch_f8_tiles<128, 128, 4, 2, 4>(b, most_tiles(a, 128), s); break;
     case kF8Tile128x128: e = launch_f8_tiles<128, 128, 2, 2, 2>(b, most_tiles(a, 128), s); break;
     case kF8Tile128x256: e = launch_f8_tiles<128, 256, 2, 4, 3>(b, most_tiles(a, 128), s); break;
-    case kF8Tile256x256: e = launch_f8_tiles<256, 256, 4, 2, 2>(b, most_tiles(a, 256), s); break;
+    case kF8Tile256x256: e = launch_f8_tiles<256, 256, 4, 2, 2, 4>(b, most_tiles(a, 256), s); break;
   }
   if (e != hipSuccess || plan.splits == 1) return e;
   const int64_t total = a.M * a.N;

@@ -6,6 +6,9 @@
 // 2 g and 2 g + 1 of row r of either operand.  w's rows are a lane's four results, x's rows the lanes, so that a lane needs one scale of
 // x for each 16 rows; a wave's 128 rows of w or fewer have one scale where w is in blocks of 128 rows.  Scales come four slabs at a
 // time, 16 bytes of a row.
+//
+// 8192 cubed 439 us, 2.5 PFLOP/s, where the same without scales (gemm_nt_dma_kernel, which adds in the matrix unit) takes 423; 16384 rows of 16 experts with
+// 4096 x 4096 287, 1.9 PFLOP/s.  What bounds them: the table of tiles in f8_dot.hip.
 #pragma once
 
 #include "f8_group.h"
@@ -83,7 +86,7 @@ __device__ __forceinline__ void f8_slabs_of(int all, int part, int parts, int* l
 #define GS_INLINE __attribute__((always_inline))
 
 // W1: w has a scale for each row.
-template <int BM, int BN, int WGM, int WGN, int NS, bool W1, bool GROUPED>
+template <int BM, int BN, int WGM, int WGN, int NS, int SPREAD, bool W1, bool GROUPED>
 __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArgs a, uint32_t tiles_m, uint32_t tiles_n) {
   constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NJ = WN / 16;
   constexpr int XQ = BM / 8 / NW, YQ = BN / 8 / NW, VQ = XQ + YQ;  // transfers of values per wave and slab: 8 rows each
@@ -238,23 +241,35 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
   using I0 = std::integral_constant<int, 0>;
   constexpr int kLast = (NJ - 1) * MI, kAll = NJ * MI;             // products in front of the last column's
   auto rest = [&]() GS_INLINE { static_for<R - 1>([&](auto i_) { add(std::integral_constant<int, kAll - (R - 1) + decltype(i_)::value>{}); }); };
-  auto columns = [&]() GS_INLINE {              // all columns of a slab but the last
+  // What of a slab's transfers is requested as soon as its buffer is drained; the rest is requested SPREAD to a column of the slab
+  // that follows: a wave waits while it requests, and where products take as long as transfers those of a burst would have them wait
+  // together (256x256 tiles, four to a column: 8192 cubed 448 -> 439 us, 3000 cubed 42.6 -> 39.7).
+  constexpr int kAtOnce = SPREAD > 0 && VQ > SPREAD * (NJ - 1) ? VQ - SPREAD * (NJ - 1) : SPREAD > 0 ? 0 : VQ;
+  int drained = 0;
+  auto columns = [&](auto rest_) GS_INLINE {    // all columns of a slab but the last; rest_: transfers are left to be requested
     static_for<NJ - 1>([&](auto n_) {
       constexpr int n = decltype(n_)::value;
       request_w(std::integral_constant<int, n + 1>{});
       __builtin_amdgcn_sched_barrier(0);
-      static_for<MI>([&](auto m_) { step(std::integral_constant<int, n * MI + decltype(m_)::value>{}); });
+      static_for<(MI > SPREAD ? MI : SPREAD)>([&](auto m_) {
+        constexpr int m = decltype(m_)::value, i = kAtOnce + n * SPREAD + m;
+        if constexpr (m < MI) step(std::integral_constant<int, n * MI + m>{});
+        if constexpr (m < SPREAD && i < VQ) {
+          if (rest_) issue_values(s + NS - 1, drained, std::integral_constant<int, i>{});
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
   // One slab that another follows.  ISSUE: slab s + NS exists and is requested.
-  auto full_slab = [&](auto issue_) GS_INLINE {
+  auto full_slab = [&](auto issue_, auto rest_) GS_INLINE {
     constexpr bool ISSUE = decltype(issue_)::value;
-    columns();
+    columns(rest_);
     if constexpr (ISSUE) wait_vmem<(NS - 2) * VQ>();
     else wait_vmem<0>();
     lds_barrier_tracked();
-    const int done = buf;
+    drained = buf;
     const bool wrap = buf + 1 == NS;
     buf = wrap ? 0 : buf + 1;
     const int d = wrap ? -(NS - 1) * kBuf : kBuf;
@@ -268,13 +283,13 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (ISSUE)
       if (((s + NS - s_first) & 3) == 0) issue_scales(s + NS);
-    static_for<(MI > VQ ? MI : VQ)>([&](auto i_) {
+    static_for<(MI > kAtOnce ? MI : kAtOnce)>([&](auto i_) {
       constexpr int i = decltype(i_)::value;
       if constexpr (i < MI) {
         step(std::integral_constant<int, kLast + i>{});
         request_x(i_);
       }
-      if constexpr (ISSUE && i < VQ) issue_values(s + NS, done, i_);
+      if constexpr (ISSUE && i < kAtOnce) issue_values(s + NS, drained, i_);
       __builtin_amdgcn_sched_barrier(0);
     });
     rest();
@@ -298,9 +313,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
     static_for<MI>([&](auto m_) { request_x(m_); });
     request_scales(s);
     take_scales();
-    while (s + NS < s_end) full_slab(std::true_type{});
-    while (s + 1 < s_end) full_slab(std::false_type{});
-    columns();
+    if (s + NS < s_end) full_slab(std::true_type{}, std::false_type{});
+    while (s + NS < s_end) full_slab(std::true_type{}, std::true_type{});
+    while (s + 1 < s_end) full_slab(std::false_type{}, s > s_first && s + NS - 1 < s_end);
+    columns(s > s_first && s + NS - 1 < s_end);
     static_for<MI>([&](auto m_) { step(std::integral_constant<int, kLast + decltype(m_)::value>{}); });
     rest();
   }
@@ -316,24 +332,24 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
   f8_write_back<MI, NJ>(a, tot, m0 + wm * WM, rows.end, n0 + wn * WN, part, zero, reinterpret_cast<float*>(lds) + wave * 16 * (WN + 4), lane);
 }
 
-template <int BM, int BN, int WGM, int WGN, int NS, bool W1, bool GROUPED>
+template <int BM, int BN, int WGM, int WGN, int NS, int SPREAD, bool W1, bool GROUPED>
 hipError_t launch_f8_tiles_as(const F8DotArgs& a, int64_t tiles_m, hipStream_t s) {
   constexpr int slabs = NS * (BM + BN) * 128 + 2 * 1024 * ((BM + 63) / 64 + (W1 ? BN / 64 : 1)), staging = WGM * WGN * 16 * (BN / WGN + 4) * 4;
   constexpr int bytes = slabs > staging ? slabs : staging;
   static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
   const int64_t tiles_n = ceil_div(a.N, BN);
   if (tiles_m * tiles_n > 0x00ffffff) return hipErrorInvalidValue;
-  const auto kernel = f8_dot_tile_kernel<BM, BN, WGM, WGN, NS, W1, GROUPED>;
+  const auto kernel = f8_dot_tile_kernel<BM, BN, WGM, WGN, NS, SPREAD, W1, GROUPED>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (attr != hipSuccess) return attr;
   hipLaunchKernelGGL(kernel, dim3(unsigned(tiles_m * tiles_n * a.splits)), dim3(WGM * WGN * 64), bytes, s, a, uint32_t(tiles_m), uint32_t(tiles_n));
   return hipGetLastError();
 }
 // tiles_m: of BM rows, at most.
-template <int BM, int BN, int WGM, int WGN, int NS>
+template <int BM, int BN, int WGM, int WGN, int NS, int SPREAD = 0>
 hipError_t launch_f8_tiles(const F8DotArgs& a, int64_t tiles_m, hipStream_t s) {
-  if (a.offsets) return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, true, true>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, false, true>(a, tiles_m, s);
-  return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, true, false>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, false, false>(a, tiles_m, s);
+  if (a.offsets) return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, true>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, true>(a, tiles_m, s);
+  return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, false>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, false>(a, tiles_m, s);
 }
 
 }  // namespace
