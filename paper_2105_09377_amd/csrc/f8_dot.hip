@@ -121,14 +121,9 @@ __global__ void __launch_bounds__(kRowWaves * 64, 2) f8_dot_rows_kernel(F8DotArg
   }
 }
 
-// Tiles of `size` rows that experts' rows are cut into, at most.
-int64_t most_tiles(const F8DotArgs& a, int64_t size) {
-  return a.offsets ? a.M / size + (a.experts < a.M ? a.experts : a.M) : ceil_div(a.M, size);
-}
-
 template <int NT, bool W1>
 hipError_t launch_rows_as(const F8DotArgs& a, hipStream_t s) {
-  const int64_t tiles_m = most_tiles(a, 16), tiles_n = ceil_div(a.N, 16 * NT);
+  const int64_t tiles_m = f8_most_tiles(a, 16), tiles_n = ceil_div(a.N, 16 * NT);
   if (tiles_m * tiles_n > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 grid(unsigned(tiles_m * tiles_n)), block(kRowWaves * 64);
   if (a.offsets) hipLaunchKernelGGL((f8_dot_rows_kernel<NT, W1, true>), grid, block, 0, s, a, uint32_t(tiles_n));
@@ -242,13 +237,13 @@ hipError_t launch_f8_dot(const F8DotArgs& given, const F8DotPlan& plan, void* wo
   switch (far ? kF8Rows2 : plan.way) {
     case kF8Rows1: e = launch_rows<1>(b, s); break;
     case kF8Rows2: e = launch_rows<2>(b, s); break;
-    case kF8Tile32x64: e = launch_f8_tiles<32, 64, 2, 2, 4>(b, most_tiles(a, 32), s); break;
-    case kF8Tile64x64: e = launch_f8_tiles<64, 64, 2, 2, 4>(b, most_tiles(a, 64), s); break;
-    case kF8Tile64x128: e = launch_f8_tiles<64, 128, 2, 4, 4>(b, most_tiles(a, 64), s); break;
-    case kF8Tile128x128Few: e = launch_f8_tiles<128, 128, 4, 2, 4>(b, most_tiles(a, 128), s); break;
-    case kF8Tile128x128: e = launch_f8_tiles<128, 128, 2, 2, 2>(b, most_tiles(a, 128), s); break;
-    case kF8Tile128x256: e = launch_f8_tiles<128, 256, 2, 4, 3>(b, most_tiles(a, 128), s); break;
-    case kF8Tile256x256: e = launch_f8_tiles<256, 256, 4, 2, 2, 4>(b, most_tiles(a, 256), s); break;
+    case kF8Tile32x64: e = launch_f8_tiles<32, 64, 2, 2, 4>(b, s); break;
+    case kF8Tile64x64: e = launch_f8_tiles<64, 64, 2, 2, 4>(b, s); break;
+    case kF8Tile64x128: e = launch_f8_tiles<64, 128, 2, 4, 4>(b, s); break;
+    case kF8Tile128x128Few: e = launch_f8_tiles<128, 128, 4, 2, 4>(b, s); break;
+    case kF8Tile128x128: e = launch_f8_tiles<128, 128, 2, 2, 2>(b, s); break;
+    case kF8Tile128x256: e = launch_f8_tiles<128, 256, 2, 4, 3>(b, s); break;
+    case kF8Tile256x256: e = launch_f8_tiles<256, 256, 4, 2, 2, 4>(b, s); break;
   }
   if (e != hipSuccess || plan.splits == 1) return e;
   const int64_t total = a.M * a.N;

@@ -332,12 +332,16 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
   f8_write_back<MI, NJ>(a, tot, m0 + wm * WM, rows.end, n0 + wn * WN, part, zero, reinterpret_cast<float*>(lds) + wave * 16 * (WN + 4), lane);
 }
 
+// Tiles of `size` rows, at most.
+inline int64_t f8_most_tiles(const F8DotArgs& a, int64_t size) {
+  return a.offsets ? a.M / size + (a.experts < a.M ? a.experts : a.M) : ceil_div(a.M, size);
+}
 template <int BM, int BN, int WGM, int WGN, int NS, int SPREAD, bool W1, bool GROUPED>
-hipError_t launch_f8_tiles_as(const F8DotArgs& a, int64_t tiles_m, hipStream_t s) {
+hipError_t launch_f8_tiles_as(const F8DotArgs& a, hipStream_t s) {
   constexpr int slabs = NS * (BM + BN) * 128 + 2 * 1024 * ((BM + 63) / 64 + (W1 ? BN / 64 : 1)), staging = WGM * WGN * 16 * (BN / WGN + 4) * 4;
   constexpr int bytes = slabs > staging ? slabs : staging;
   static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
-  const int64_t tiles_n = ceil_div(a.N, BN);
+  const int64_t tiles_m = f8_most_tiles(a, BM), tiles_n = ceil_div(a.N, BN);
   if (tiles_m * tiles_n > 0x00ffffff) return hipErrorInvalidValue;
   const auto kernel = f8_dot_tile_kernel<BM, BN, WGM, WGN, NS, SPREAD, W1, GROUPED>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -345,11 +349,13 @@ hipError_t launch_f8_tiles_as(const F8DotArgs& a, int64_t tiles_m, hipStream_t s
   hipLaunchKernelGGL(kernel, dim3(unsigned(tiles_m * tiles_n * a.splits)), dim3(WGM * WGN * 64), bytes, s, a, uint32_t(tiles_m), uint32_t(tiles_n));
   return hipGetLastError();
 }
-// tiles_m: of BM rows, at most.
 template <int BM, int BN, int WGM, int WGN, int NS, int SPREAD = 0>
-hipError_t launch_f8_tiles(const F8DotArgs& a, int64_t tiles_m, hipStream_t s) {
-  if (a.offsets) return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, true>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, true>(a, tiles_m, s);
-  return a.w_rows == 1 ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, false>(a, tiles_m, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, false>(a, tiles_m, s);
+hipError_t launch_f8_tiles(const F8DotArgs& a, hipStream_t s) {
+  if (a.w_rows != 1)
+    return a.offsets ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, true>(a, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, false, false>(a, s);
+  // (scales for each row of w need more registers than the largest tile leaves)
+  if constexpr (BM * BN > 128 * 256) return launch_f8_tiles<128, 256, 2, 4, 3>(a, s);
+  else return a.offsets ? launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, true>(a, s) : launch_f8_tiles_as<BM, BN, WGM, WGN, NS, SPREAD, true, false>(a, s);
 }
 
 }  // namespace
