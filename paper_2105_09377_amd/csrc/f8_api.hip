@@ -172,6 +172,7 @@ int check_result(const gs_ap* out, int act) {
 }
 
 int run_dot(F8DotArgs& a, gs_ap* out, int act, void* workspace, size_t workspace_bytes, void* stream) {
+  if (a.offsets && a.experts == 0) return GS_OK;      // (every row is nobody's)
   a.out = out->data;
   a.out_dtype = out->dtype;
   a.relu = act == GS_ACT_RELU;
@@ -318,7 +319,7 @@ int glenside_f8_expert_dot(const gs_f8* a0, const gs_ap* tokens, const gs_ap* of
 
 size_t glenside_f8_expert_dot_workspace(const gs_f8* a0, int64_t rows, const gs_f8* a1) {
   F8DotArgs a;
-  return rows < 0 || expert_args(a0, rows, a1, false, &a) ? 0 : plan_f8_dot(a.M, a.N, a.K, a.experts).part_bytes;
+  return rows < 0 || expert_args(a0, rows, a1, false, &a) || a.experts == 0 ? 0 : plan_f8_dot(a.M, a.N, a.K, a.experts).part_bytes;
 }
 
 size_t glenside_expert_sort_workspace(int64_t choices, int64_t n_experts) {

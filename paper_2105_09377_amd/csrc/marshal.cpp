@@ -772,6 +772,22 @@ PyObject* py_mx4_attend(PyObject*, PyObject* const* p, Py_ssize_t n) {
   });
 }
 
+// New tensors that are made and dropped together, in one allocation: each costs the caller a microsecond.
+struct Together {
+  at::Tensor bytes;
+  size_t used = 0;
+  Together(size_t total, const at::Tensor& like) : bytes(at::empty({int64_t(total)}, at::TensorOptions().dtype(at::kByte).device(like.device()))) {}
+  static size_t room(size_t n) { return (n + 511) / 512 * 512; }      // (as aligned as allocations are)
+  at::Tensor take(at::IntArrayRef sizes, at::ScalarType type) {
+    const size_t item = c10::elementSize(type);
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_storage_offset(int64_t(used / item));
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    used += room(size_t(t.numel()) * item);
+    return t;
+  }
+};
+
 // binding.F8: (values, scales, shape, n_access, block_rows)
 struct F8 {
   at::Tensor values, scales;
@@ -785,30 +801,34 @@ struct F8 {
     d.scales = scales.data_ptr();
     const Ints shape(item(o, 2, 5, "an F8"));
     pattern(shape.v, shape.n, integer(item(o, 3, 5, "an F8")), integer(item(o, 4, 5, "an F8")));
-    size_t need_values = 0, need_scales = 0;
-    call("f8_sizes", [&] { return api.f8_sizes(&d, &need_values, &need_scales); });
+    sizes();
     if (size_t(values.numel()) < need_values || size_t(scales.numel()) * 4 < need_scales) refuse(GS_ERR_SHAPE, "F8");
     same_device(values, {&scales});
   }
   // New storage for a pattern.
   F8(const int64_t* shape, int64_t rank, int64_t n_access, int64_t block_rows, const at::Tensor& like) {
     pattern(shape, rank, n_access, block_rows);
-    size_t need_values = 0, need_scales = 0;
-    call("f8_sizes", [&] { return api.f8_sizes(&d, &need_values, &need_scales); });
+    sizes();
     int64_t cols = 1, v[GS_MAX_RANK + 2];
     for (int64_t i = n_access; i < rank; ++i) cols *= shape[i];
     for (int64_t i = 0; i < n_access; ++i) v[i] = shape[i];
     v[n_access] = (cols + 127) / 128;
     v[n_access + 1] = 128;
-    values = at::empty(at::IntArrayRef(v, size_t(n_access) + 2), at::TensorOptions().dtype(at::kFloat8_e4m3fn).device(like.device()));
+    Together both(Together::room(need_values) + need_scales, like);
+    values = both.take(at::IntArrayRef(v, size_t(n_access) + 2), at::kFloat8_e4m3fn);
     if (n_access > 0) v[n_access - 1] = (v[n_access - 1] + block_rows - 1) / block_rows;
     v[n_access] = (v[n_access] + 3) / 4 * 4;
-    scales = at::empty(at::IntArrayRef(v, size_t(n_access) + 1), at::TensorOptions().dtype(at::kFloat).device(like.device()));
+    scales = both.take(at::IntArrayRef(v, size_t(n_access) + 1), at::kFloat);
     d.values = values.data_ptr();
     d.scales = scales.data_ptr();
   }
 
  private:
+  size_t need_values = 0, need_scales = 0;
+  void sizes() {
+    const int status = api.f8_sizes(&d, &need_values, &need_scales);
+    if (status != GS_OK) refuse(status, "F8");
+  }
   void pattern(const int64_t* shape, int64_t rank, int64_t n_access, int64_t block_rows) {
     if (rank > GS_MAX_RANK) {
       PyErr_SetString(PyExc_ValueError, "rank above GS_MAX_RANK");
@@ -943,7 +963,8 @@ PyObject* py_expert_sort(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded(n, 4, [&](PyObject*& r) {
     const at::Tensor& experts = tensor(p[0]);
     const int64_t n_experts = integer(p[1]);
-    if (n_experts < 0 || n_experts > (int64_t(1) << 30)) refuse(GS_ERR_SHAPE, "expert_sort");
+    if (n_experts < 0) refuse(GS_ERR_SHAPE, "expert_sort");
+    if (n_experts > 4096) refuse(GS_ERR_UNSUPPORTED, "expert_sort");    // (before offsets for them are made)
     at::Tensor offsets, tokens, places;
     if (p[2] != Py_None) {
       offsets = tensor(item(p[2], 0, 3, "an ExpertSort"));
@@ -951,10 +972,11 @@ PyObject* py_expert_sort(PyObject*, PyObject* const* p, Py_ssize_t n) {
       places = tensor(item(p[2], 2, 3, "an ExpertSort"));
       if (offsets.dim() == 1 && offsets.size(0) != n_experts + 1) refuse(GS_ERR_SHAPE, "expert_sort");
     } else {
-      const auto ints = at::TensorOptions().dtype(at::kInt).device(experts.device());
-      offsets = at::empty({n_experts + 1}, ints);
-      tokens = at::empty({experts.numel()}, ints);
-      places = at::empty(experts.sizes(), ints);
+      const size_t all = size_t(experts.numel()) * 4;
+      Together three(Together::room(size_t(n_experts + 1) * 4) + Together::room(all) + all, experts);
+      offsets = three.take({n_experts + 1}, at::kInt);
+      tokens = three.take({experts.numel()}, at::kInt);
+      places = three.take(experts.sizes(), at::kInt);
     }
     const gs_ap ea = describe_all(experts);
     gs_ap oa = describe_all(offsets), ta = describe_all(tokens), pa = describe_all(places);

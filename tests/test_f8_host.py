@@ -113,6 +113,8 @@ def test_products_want_their_workspace():
     assert L.glenside_f8_dot_workspace(ref(f8((64, 8191), 1)), ref(a1)) == 0
     assert L.glenside_f8_dot_workspace(None, ref(a1)) == 0
     assert L.glenside_f8_expert_dot_workspace(ref(a0), 64, ref(f8((4, 128, 8192), 2, 128))) == 0
+    assert L.glenside_f8_expert_dot_workspace(ref(a0), 64, ref(f8((0, 8192, 8192), 2, 128))) == 0
+    assert L.glenside_f8_expert_dot_workspace(ref(a0), -1, ref(f8((4, 128, 8192), 2, 128))) == 0
 
 
 def experts_dot(**kw):
@@ -132,6 +134,12 @@ def experts_dot(**kw):
 def test_experts_products_refuse(kw, status):
     a = experts_dot(**kw)
     assert gs.lib().glenside_f8_expert_dot(ref(a["a0"]), ref(a["tokens"]), ref(a["offsets"]), ref(a["w"]), ref(a["out"]), a["act"], None, 0, None) == status
+
+
+def test_no_experts_launch_nothing():
+    """Not even where as many rows of one matrix would share sums in a workspace."""
+    a = experts_dot(a0=f8((64, 8192), 1), w=f8((0, 8192, 8192), 2, 128), offsets=ap((1,), 1, I32), tokens=None, out=ap((64, 8192), 2, F32))
+    assert gs.lib().glenside_f8_expert_dot(ref(a["a0"]), None, ref(a["offsets"]), ref(a["w"]), ref(a["out"]), 0, None, 0, None) == gs.GS_OK
 
 
 def sort(**kw):
@@ -243,6 +251,7 @@ def test_binding_refuses_experts():
     refused(gs.GS_ERR_DTYPE, gs.expert_sort, e.float(), 4)
     refused(gs.GS_ERR_SHAPE, gs.expert_sort, e, -1)
     refused(gs.GS_ERR_UNSUPPORTED, gs.expert_sort, e, 5000)
+    refused(gs.GS_ERR_UNSUPPORTED, gs.expert_sort, e, 1 << 40)
     refused(gs.GS_ERR_RANK, gs.expert_sort, e[0].contiguous(), 4)
     three = gs.ExpertSort(torch.zeros(5, dtype=torch.int32), torch.zeros(8, dtype=torch.int32), e.clone())
     refused(gs.GS_ERR_SHAPE, gs.expert_sort, e, 3, out=three)

@@ -163,11 +163,11 @@ def test_no_choices():
 # ------------------------------------------------------------------------------------------------
 
 
-def check_experts(tokens, choices, experts, n, k, gather, w_rows=128, odt=BF, act=gs.GS_ACT_NONE, dropped=0.1, e=None):
+def check_experts(tokens, choices, experts, n, k, gather, w_rows=128, odt=BF, act=gs.GS_ACT_NONE, dropped=0.1, e=None, x_rows=1):
     e = chosen(tokens, choices, experts, n + k, dropped) if e is None else e
     offsets, of, _ = f8.sort(e.numpy(), experts)
     rows = e.numel()
-    x, xv = operand((tokens if gather else rows, k), 1, 1, 1)
+    x, xv = operand((tokens if gather else rows, k), 1, x_rows, 1)
     w, wv = operand((experts, n, k), 2, w_rows, 2)
     before = normal((rows, n), 3, odt)
     got = gs.f8_expert_dot(x, w, torch.from_numpy(offsets).to(I32).to(DEV), tokens=torch.from_numpy(of).to(I32).to(DEV) if gather else None,
@@ -191,6 +191,8 @@ def test_expert_dot(tokens, choices, experts, n, k, gather):
 def test_expert_dot_kinds(tokens):
     check_experts(tokens, 2, 4, 300, 200, True, w_rows=1, odt=F32)
     check_experts(tokens, 2, 4, 300, 200, False, act=gs.GS_ACT_RELU)
+    check_experts(tokens, 2, 4, 140, 700, True, x_rows=128)
+    check_experts(tokens, 2, 4, 140, 700, False, x_rows=128, w_rows=1)
 
 
 @pytest.mark.parametrize("tokens", [9, 700])
@@ -227,6 +229,13 @@ def test_expert_dot_nan_stays_in_its_row():
         got = gs.f8_expert_dot(xq, w, torch.tensor([0, rows // 2, rows], dtype=I32, device=DEV), tokens=tokens.to(I32).to(DEV)).cpu()
         assert torch.equal(torch.isnan(got).all(1), tokens == 2) and torch.equal(torch.isnan(got).any(1), tokens == 2)
         assert (got[tokens < 0] == 0).all()
+
+
+def test_no_experts():
+    x, out = operand((64, 200), 1, 1, 1)[0], torch.ones(64, 70, device=DEV)
+    w = gs.F8(torch.zeros(0, 70, 2, 128, dtype=torch.uint8, device=DEV), torch.zeros(0, 1, 4, device=DEV), (0, 70, 200), 2, 128)
+    gs.f8_expert_dot(x, w, torch.zeros(1, dtype=I32, device=DEV), out=out)
+    assert (out == 1).all()
 
 
 def test_no_rows_and_no_tokens():

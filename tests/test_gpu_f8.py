@@ -88,6 +88,26 @@ def test_quantize_matrices(block_rows):
     assert np.array_equal(to_oracle(got).reshape(3, 130, 160), f8.round32(f8.dequantize(code, scales, 160, block_rows)))
 
 
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("shape", [(), (5,), (300,), (3, 100)])
+def test_quantize_one_element(shape, block_rows):
+    """Every dimension a compute dimension; a number by itself."""
+    x = normal(shape, 7, F32) if shape else torch.tensor(-3.7)
+    m = gs.f8_quantize(x.to(DEV), n_access=0, block_rows=block_rows)
+    code, scales = f8.quantize(to_oracle(x).reshape(1, 1, -1), block_rows)
+    assert m.values.shape == code.shape[2:] and np.array_equal(codes_of(m), code[0, 0])
+    same_scales(m.scales, scales[0, 0])
+    assert np.array_equal(to_oracle(gs.f8_dequantize(m, out_dtype=F32)).reshape(-1), f8.round32(f8.dequantize(code, scales, x.numel(), block_rows))[0, 0])
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_nothing(block_rows):
+    for shape in ((0, 64), (4, 0), (0, 0), (2, 0, 5), (0, 3, 5)):
+        m = gs.f8_quantize(torch.zeros(shape, device=DEV), block_rows=block_rows)
+        assert m.values.numel() == 0 and gs.f8_dequantize(m).shape == shape
+        assert gs.norm(torch.zeros(shape, device=DEV))[0].shape == shape and gs.f8_norm(torch.zeros(shape, device=DEV))[0].shape == shape
+
+
 def test_quantize_many():
     """More pieces than a lane's first, rows of every alignment."""
     for rows, cols, dtype in ((4100, 1025, BF), (2051, 2050, F32)):
@@ -327,6 +347,22 @@ def test_dot_dimensions():
     want, size = xv[0] @ wv.reshape(256, 200).T, np.abs(xv[0]) @ np.abs(wv.reshape(256, 200)).T
     assert got.shape == (5, 2, 128)
     within(got.reshape(5, 256), want, allowed(size, want, 2, F32))
+
+
+@pytest.mark.parametrize("m", [2, 40])
+def test_dot_of_the_longest_rows(m):
+    """Beyond 2^22 numbers, where few of them are not zero: sums are exact."""
+    k, n = (1 << 22) + 300, 33
+    blocks = -(-k // 128)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, w = (torch.where(torch.rand(r, k, generator=g, device=DEV) < 2e-3, torch.randint(-3, 4, (r, k), generator=g, device=DEV).float(), 0.0) for r in (m, n))
+    x[:, -1], w[:, -1] = 2.0, 3.0
+
+    def held(t):
+        codes = torch.nn.functional.pad(t, (0, blocks * 128 - k)).to(torch.float8_e4m3fn).view(t.shape[0], blocks, 128)
+        return gs.F8(codes, torch.ones(t.shape[0], -(-blocks // 4) * 4, device=DEV), tuple(t.shape), 1, 1)
+
+    assert torch.equal(gs.f8_dot(held(x), held(w)), x @ w.t().contiguous())
 
 
 @pytest.mark.parametrize("m", [3, 300])
