@@ -325,8 +325,9 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
     }
     if constexpr (OUT == GS_F8) {
       // (what a row has behind its end is zero: infinities of r must not make it NaN)
+      if (left < 8)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = i < left ? h[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) h[i] = i < left ? h[i] : 0.0f;
       const float scale = f8_scale(f8_block_top(h));
       if (piece >= pieces) return;
       static_cast<i32x2*>(a.out)[row * pieces + piece] = f8_encode8(h, scale);

@@ -135,27 +135,37 @@ hipError_t launch_rows(const F8DotArgs& a, hipStream_t s) {
   return a.w_rows == 1 ? launch_rows_as<NT, true>(a, s) : launch_rows_as<NT, false>(a, s);
 }
 
-// Adds the parts of a sum over K, in their order: four results per lane.
+// Adds the SPLITS parts of a sum over K, in their order: four results per lane, whose parts are all under way together.
 typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int SPLITS>
 __global__ void __launch_bounds__(256) f8_dot_join_kernel(const float* parts, F8DotArgs a, int64_t total) {
   const int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (at >= total) return;
+  f32x4 part[SPLITS];
   if (at + 4 <= total) {
-    f32x4 sum = *reinterpret_cast<const f32x4_any4*>(parts + at);
-    for (int p = 1; p < a.splits; ++p) sum += *reinterpret_cast<const f32x4_any4*>(parts + p * total + at);
-    if (a.relu)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = fmaxf(sum[e], 0.0f);
+    for (int p = 0; p < SPLITS; ++p) part[p] = *reinterpret_cast<const f32x4_any4*>(parts + p * total + at);
+  } else {
+#pragma unroll
+    for (int p = 0; p < SPLITS; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[p][e] = at + e < total ? parts[p * total + at + e] : 0.0f;
+  }
+  f32x4 sum = part[0];
+#pragma unroll
+  for (int p = 1; p < SPLITS; ++p) sum += part[p];
+  if (a.relu)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaxf(sum[e], 0.0f);
+  if (at + 4 <= total) {
     if (a.out_dtype == GS_BF16)
       *reinterpret_cast<i32x2*>(static_cast<uint16_t*>(a.out) + at) = i32x2{int32_t(pack_bf16x2(sum[0], sum[1])), int32_t(pack_bf16x2(sum[2], sum[3]))};
     else *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = sum;
     return;
   }
-  for (int64_t i = at; i < total; ++i) {
-    float sum = parts[i];
-    for (int p = 1; p < a.splits; ++p) sum += parts[p * total + i];
-    store_result<float>(a.out, nullptr, a.out_dtype, i, sum, a.relu);
-  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (at + e < total) store_result<float>(a.out, nullptr, a.out_dtype, at + e, sum[e], 0);
 }
 
 int64_t tiles(int64_t M, int64_t N, int bm, int bn) { return ceil_div(M, bm) * ceil_div(N, bn); }
@@ -248,8 +258,11 @@ hipError_t launch_f8_dot(const F8DotArgs& given, const F8DotPlan& plan, void* wo
   if (e != hipSuccess || plan.splits == 1) return e;
   const int64_t total = a.M * a.N;
   if (ceil_div(total, 1024) > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(f8_dot_join_kernel, dim3(unsigned(ceil_div(total, 1024))), dim3(256), 0, s, static_cast<const float*>(workspace), a, total);
-  return hipGetLastError();
+  const auto join = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(ceil_div(total, 1024))), dim3(256), 0, s, static_cast<const float*>(workspace), a, total);
+    return hipGetLastError();
+  };
+  return plan.splits == 2 ? join(f8_dot_join_kernel<2>) : plan.splits == 4 ? join(f8_dot_join_kernel<4>) : join(f8_dot_join_kernel<8>);
 }
 
 }  // namespace gs

@@ -2,8 +2,9 @@
 //
 // A slab is 128 bytes of K per row, one block: a 16x16x128 product takes 16 rows of each operand and gives the block's sums, which
 // vector instructions, times the two scales, add to the results.  Rows are 128 bytes in LDS, their 16-byte columns exchanged by an
-// XOR of the row so that the 16 rows that are read together fall on different banks; lane (r = lane % 16, g = lane / 16) has columns
-// 2 g and 2 g + 1 of row r of either operand.  w's rows are a lane's four results, x's rows the lanes, so that a lane needs one scale of
+// XOR of the row so that lanes that are served together fall on different banks; lane (r = lane % 16, g = lane / 16) has columns
+// g and g + 4 of row r of either operand (with 2 g and 2 g + 1 lanes 4 to 11 of one g meet those of the next on a bank: 4.3 cycles more a
+// read).  w's rows are a lane's four results, x's rows the lanes, so that a lane needs one scale of
 // x for each 16 rows; a wave's 128 rows of w or fewer have one scale where w is in blocks of 128 rows.  Scales come four slabs at a
 // time, 16 bytes of a row.
 //
@@ -172,11 +173,11 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
   f32x4 tot[MI][NJ];
   static_for<MI>([&](auto m_) { static_for<NJ>([&](auto n_) { tot[decltype(m_)::value][decltype(n_)::value] = f32x4{0, 0, 0, 0}; }); });
 
-  // fragment addresses in the buffer being read: columns 2 g and 2 g + 1 of row lane % 16
+  // fragment addresses in the buffer being read: columns g and g + 4 of row lane % 16
   const uint8_t *xa[2], *ya[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const int col = ((2 * (lane >> 4) + c) ^ (((lane & 15) / 2) % 8)) * 16;
+    const int col = (((lane >> 4) + 4 * c) ^ (((lane & 15) / 2) % 8)) * 16;
     xa[c] = lds + (wm * WM + (lane & 15)) * 128 + col;
     ya[c] = lds + kX + (wn * WN + (lane & 15)) * 128 + col;
   }
