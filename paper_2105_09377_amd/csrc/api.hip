@@ -38,6 +38,15 @@ int launch_status(hipError_t e) {
   return GS_ERR_LAUNCH;
 }
 
+bool overlaps(const gs_ap* a, const gs_ap* b) {
+  uint64_t na = dtype_size(a->dtype), nb = dtype_size(b->dtype);
+  for (int i = 0; i < a->rank; ++i) na *= uint64_t(a->shape[i]);
+  for (int i = 0; i < b->rank; ++i) nb *= uint64_t(b->shape[i]);
+  if (na == 0 || nb == 0) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a->data), pb = reinterpret_cast<uintptr_t>(b->data);
+  return pa < pb + nb && pb < pa + na;
+}
+
 }  // namespace gs
 
 namespace {
@@ -57,14 +66,6 @@ bool same_shape(const gs_ap* a, const gs_ap* b) {
   for (int i = 0; i < a->rank; ++i)
     if (a->shape[i] != b->shape[i]) return false;
   return true;
-}
-
-// Do the bytes of two access patterns overlap?  (Empty tensors overlap nothing.)
-bool overlaps(const gs_ap* a, const gs_ap* b) {
-  const uint64_t na = uint64_t(numel(a)) * dtype_size(a->dtype), nb = uint64_t(numel(b)) * dtype_size(b->dtype);
-  if (na == 0 || nb == 0) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a->data), pb = reinterpret_cast<uintptr_t>(b->data);
-  return pa < pb + nb && pb < pa + na;
 }
 
 uint32_t lowest_bits(int dtype) {

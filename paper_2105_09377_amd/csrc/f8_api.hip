@@ -6,6 +6,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <initializer_list>
+
 using namespace gs;
 
 namespace {
@@ -60,6 +62,14 @@ bool same_pattern_shape(const A* a, const B* b) {
   for (int i = 0; i < a->rank; ++i)
     if (a->shape[i] != b->shape[i]) return false;
   return true;
+}
+
+// Does any of the results share bytes with any of the inputs?  Each may be NULL.
+bool shares(std::initializer_list<const gs_ap*> results, std::initializer_list<const gs_ap*> inputs) {
+  for (const gs_ap* r : results)
+    for (const gs_ap* in : inputs)
+      if (r && in && overlaps(r, in)) return true;
+  return false;
 }
 
 bool is_float(int dtype) { return dtype == GS_BF16 || dtype == GS_F32; }
@@ -253,6 +263,7 @@ int glenside_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight, fl
   if (out->rank != x->rank || out->n_access != x->n_access) return GS_ERR_RANK;
   if (!same_pattern_shape(out, x)) return GS_ERR_SHAPE;
   if (!is_float(out->dtype)) return GS_ERR_DTYPE;
+  if (shares({sum, out}, {x, residual, weight})) return GS_ERR_UNSUPPORTED;
   a.out = out->data;
   a.out_dtype = out->dtype;
   return launch_status(launch_norm(a, static_cast<hipStream_t>(stream)));
@@ -267,7 +278,7 @@ int glenside_f8_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight,
   if (st) return st;
   if (out->rank != x->rank || out->n_access != x->n_access) return GS_ERR_RANK;
   if (!same_pattern_shape(out, x)) return GS_ERR_SHAPE;
-  if (out->block_rows != 1) return GS_ERR_UNSUPPORTED;
+  if (out->block_rows != 1 || shares({sum}, {x, residual, weight})) return GS_ERR_UNSUPPORTED;
   a.out = out->values;
   a.scales = static_cast<float*>(out->scales);
   a.out_dtype = GS_F8;
@@ -345,6 +356,7 @@ int glenside_expert_sort(const gs_ap* experts, gs_ap* offsets, gs_ap* tokens, gs
   if (a.n > (int64_t(1) << 30) || a.choices > (int64_t(1) << 30) || a.n_experts > 4096) return GS_ERR_UNSUPPORTED;
   const size_t need = expert_sort_workspace(a.n, a.n_experts);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return GS_ERR_WORKSPACE;
+  if (shares({offsets, tokens, places}, {experts})) return GS_ERR_UNSUPPORTED;
   a.experts = static_cast<const int32_t*>(experts->data);
   a.offsets = static_cast<int32_t*>(offsets->data);
   a.tokens = static_cast<int32_t*>(tokens->data);
@@ -358,6 +370,7 @@ int glenside_expert_split(const gs_ap* x, const gs_ap* places, gs_ap* rows, void
   const int st = rows_args(x, rows, places, nullptr, &a);
   if (st) return st;
   if (x->dtype != rows->dtype) return GS_ERR_DTYPE;
+  if (shares({rows}, {x, places})) return GS_ERR_UNSUPPORTED;
   a.flat = x->data;
   a.rows_out = rows->data;
   a.dtype = x->dtype;
@@ -369,6 +382,7 @@ int glenside_expert_join(const gs_ap* rows, const gs_ap* places, const gs_ap* we
   const int st = rows_args(out, rows, places, weights, &a);
   if (st) return st;
   if (!is_float(rows->dtype) || !is_float(out->dtype)) return GS_ERR_DTYPE;
+  if (shares({out}, {rows, places, weights})) return GS_ERR_UNSUPPORTED;
   a.flat_out = out->data;
   a.rows = rows->data;
   a.dtype = rows->dtype;
@@ -394,6 +408,7 @@ int glenside_expert_join_grad(const gs_ap* grad, const gs_ap* rows, const gs_ap*
     if (!same_pattern_shape(grad_weights, places)) return GS_ERR_SHAPE;
     a.grad_weights = static_cast<float*>(grad_weights->data);
   }
+  if (shares({grad_rows, grad_weights}, {grad, rows, places, weights})) return GS_ERR_UNSUPPORTED;
   a.flat = grad->data;
   a.rows = rows->data;
   a.rows_out = grad_rows->data;

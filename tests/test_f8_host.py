@@ -204,6 +204,40 @@ def test_rows_refuse_types_and_weights():
         assert L.glenside_expert_join_grad(a["flat"], a["rows"], a["places"], a["weights"], a["grad_rows"], a["grad_weights"], None) == status
 
 
+def at(place, shape, n_access, dtype=BF):
+    """A pattern in a megabyte of its own."""
+    return ap(shape, n_access, dtype, data=FAKE + place * (1 << 20))
+
+
+def test_nothing_works_in_place():
+    """A result that shares bytes with an input, from its first or only its last, is refused; norms of long rows read their inputs twice."""
+    L, no = gs.lib(), gs.GS_ERR_UNSUPPORTED
+    x, residual, weight, total, out = at(1, (4, 64), 1), at(2, (4, 64), 1), at(3, (64,), 0), at(4, (4, 64), 1), at(5, (4, 64), 1)
+    codes = f8((4, 64), 1, values=FAKE + (9 << 20), scales=FAKE + (10 << 20))
+    for of in (x, residual, weight):
+        for back in (0, 4 * 64 * 2 - 16):
+            onto = ap((4, 64), 1, data=of.data - back)
+            args = [ref(x), ref(residual), ref(weight), 1e-6]
+            assert L.glenside_norm(*args, ref(onto), ref(out), None) == no
+            assert L.glenside_norm(*args, ref(total), ref(onto), None) == no
+            assert L.glenside_f8_norm(*args, ref(onto), ref(codes), None) == no
+    experts, offsets = at(1, (10, 3), 2, I32), at(2, (5,), 1, I32)
+    tokens, places = at(3, (30,), 1, I32), at(4, (10, 3), 2, I32)
+    for three in ((ap((5,), 1, I32, data=experts.data), tokens, places), (offsets, ap((30,), 1, I32, data=experts.data), places),
+                  (offsets, tokens, ap((10, 3), 2, I32, data=experts.data - 112))):
+        assert L.glenside_expert_sort(ref(experts), *(ref(t) for t in three), None, 0, None) == no
+    flat, rows_, weights = at(1, (10, 40), 1), at(2, (30, 40), 1), at(5, (10, 3), 2, F32)
+    grad_rows, grad_weights = at(6, (30, 40), 1), at(7, (10, 3), 2, F32)
+    for of in (flat, places):
+        assert L.glenside_expert_split(ref(flat), ref(places), ref(ap((30, 40), 1, data=of.data)), None) == no
+    for of in (rows_, places, weights):
+        assert L.glenside_expert_join(ref(rows_), ref(places), ref(weights), ref(ap((10, 40), 1, data=of.data)), None) == no
+    for of in (flat, rows_, places, weights):
+        args = [ref(flat), ref(rows_), ref(places), ref(weights)]
+        assert L.glenside_expert_join_grad(*args, ref(ap((30, 40), 1, data=of.data)), ref(grad_weights), None) == no
+        assert L.glenside_expert_join_grad(*args, ref(grad_rows), ref(ap((10, 3), 2, F32, data=of.data)), None) == no
+
+
 def refused(status, call, *args, **kw):
     with pytest.raises(gs.GlensideError) as e:
         call(*args, **kw)

@@ -210,6 +210,20 @@ def test_norm(cols, dtype, wdt):
         same_scales(m.scales, scales[0])
 
 
+@pytest.mark.parametrize("cols", [32768, 32769, 50007])
+def test_norm_of_several_long_rows(cols):
+    """Rows that registers hold no longer are read twice."""
+    x, res, w = normal((5, cols), 1), normal((5, cols), 2), normal((cols,), 3, F32)
+    h = (x.float() + res.float()).to(BF)
+    want = f8.norm(to_oracle(h), to_oracle(w), np.float64(np.float32(1e-5)))
+    got, total = gs.norm(x.to(DEV), w.to(DEV), residual=res.to(DEV), eps=1e-5, out_dtype=F32)
+    assert torch.equal(total.cpu(), h) and torch.equal(got.cpu(), torch.from_numpy(f8.round32(want)).to(F32))
+    m, total = gs.f8_norm(x.to(DEV), w.to(DEV), residual=res.to(DEV), eps=1e-5)
+    code, scales = f8.quantize(f8.round32(want)[None])
+    assert torch.equal(total.cpu(), h) and np.array_equal(codes_of(m), code[0])
+    same_scales(m.scales, scales[0])
+
+
 def test_norm_is_that_of_the_sum_as_stored():
     x, res, w = normal((17, 1000), 1).to(DEV), normal((17, 1000), 2).to(DEV), normal((1000,), 3).to(DEV)
     total = gs.pair_reduce(x, res)
