@@ -465,8 +465,8 @@ int glenside_expert_join_grad(const gs_ap* grad, const gs_ap* rows, const gs_ap*
 /* The experts' products: out[r] = compute dotProd (cartProd a0[tokens[r]] a1[e]) for the rows r of every expert e.  a0
  * ((T),(k..)) F8, tokens i32 ((M),()) (NULL: row r is of a0's row r, M = T; a row whose token is none of 0 .. T - 1 becomes
  * zeros), offsets i32 ((E + 1),()) as _sort gives them, a1 ((E, N),(k..)) F8, out ((M, N),()) bf16 or f32; rows
- * of no expert stay as they were.  Sums as in glenside_f8_dot.  Offsets are taken as at least 0, at most M, and none as below the one
- * before; where they name a row twice, its results race.
+ * of no expert stay as they were.  Sums as in glenside_f8_dot.  Offsets are taken as at least 0, at most M, and none as below one
+ * before it: no row is two experts'.
  * workspace: glenside_f8_expert_dot_workspace(a0, M, a1) bytes (may be 0; 16-byte aligned).           */
 int glenside_f8_expert_dot(const gs_f8* a0, const gs_ap* tokens, const gs_ap* offsets, const gs_f8* a1, gs_ap* out,
                            int act, void* workspace, size_t workspace_bytes, void* stream);

@@ -112,12 +112,13 @@ def expert_dot(x, tokens, offsets, w, out):
     out = out.copy()
     size = np.zeros_like(out)
     m = len(out)
+    lo = min(max(int(offsets[0]), 0), m)
     for e in range(len(w)):
-        lo = min(max(int(offsets[e]), 0), m)
-        hi = max(lo, min(int(offsets[e + 1]), m))
+        hi = max(lo, min(int(offsets[e + 1]), m))            # (no offset is taken as below one before it)
         for r in range(lo, hi):
             t = r if tokens is None else int(tokens[r])
             row = x[t] if 0 <= t < len(x) else np.zeros(w.shape[2])
             out[r] = w[e] @ row
             size[r] = np.abs(w[e]) @ np.abs(row)
+        lo = hi
     return out, size

@@ -22,22 +22,40 @@ __device__ __forceinline__ int32_t lanes_up_to(int32_t v, int lane) {
   return v;
 }
 
-// Expert e's rows of M, whatever the offsets are.
-__device__ __forceinline__ void f8_rows_of(const F8DotArgs& a, int64_t e, int64_t* lo, int64_t* hi) {
-  const int64_t l = a.offsets[e], h = a.offsets[e + 1];
-  *lo = l < 0 ? 0 : l < a.M ? l : a.M;
-  *hi = h < *lo ? *lo : h < a.M ? h : a.M;
+// The rows of 64 experts from e0 on, one's to a lane (none behind the last expert): offsets are taken as at least 0, at most M and none as
+// below one before it, so that no row is two experts' and there are no more tiles than f8_most_tiles says.  `most` is the largest offset before
+// e0, and then that before e0 + 64.  Offsets that go up, as sorting gives them, are used as they are.
+__device__ __forceinline__ void f8_rows_of(const F8DotArgs& a, int64_t e0, int lane, int32_t* most, int32_t* lo, int32_t* hi) {
+  const int64_t e = e0 + lane < a.experts ? e0 + lane : a.experts, next = e < a.experts ? e + 1 : e;
+  int32_t l = a.offsets[e], h = a.offsets[next];
+  const int32_t m = int32_t(a.M);
+  l = l < 0 ? 0 : l < m ? l : m;
+  h = h < 0 ? 0 : h < m ? h : m;
+  if (__ballot(l < *most || h < l)) {
+    if (lane == 0) l = l > *most ? l : *most;
+    if (lane == 0) h = h > l ? h : l;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int32_t o = __shfl_up(h, d);
+      h = lane >= d && o > h ? o : h;
+    }
+    const int32_t o = __shfl_up(h, 1);
+    l = lane == 0 ? l : o;
+  }
+  *most = __builtin_amdgcn_readlane(h, 63);
+  *lo = l;
+  *hi = h;
 }
 
 // How many tiles of `size` rows the experts' rows are cut into, expert by expert.
 __device__ __forceinline__ int64_t f8_group_tiles(const F8DotArgs& a, int size) {
   const int lane = threadIdx.x & 63;
   int64_t all = 0;
+  int32_t most = 0;
   for (int64_t e0 = 0; e0 < a.experts; e0 += 64) {
-    const int64_t e = e0 + lane;
-    int64_t lo = 0, hi = 0;
-    if (e < a.experts) f8_rows_of(a, e, &lo, &hi);
-    all += __builtin_amdgcn_readlane(lanes_up_to(int32_t((hi - lo + size - 1) / size), lane), 63);
+    int32_t lo, hi;
+    f8_rows_of(a, e0, lane, &most, &lo, &hi);
+    all += __builtin_amdgcn_readlane(lanes_up_to((hi - lo + size - 1) / size, lane), 63);
   }
   return all;
 }
@@ -46,11 +64,11 @@ __device__ __forceinline__ int64_t f8_group_tiles(const F8DotArgs& a, int size) 
 __device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile, int size) {
   const int lane = threadIdx.x & 63;
   int64_t before = 0;
+  int32_t most = 0;
   for (int64_t e0 = 0; e0 < a.experts; e0 += 64) {
-    const int64_t e = e0 + lane;
-    int64_t lo = 0, hi = 0;
-    if (e < a.experts) f8_rows_of(a, e, &lo, &hi);
-    const int32_t tiles = int32_t((hi - lo + size - 1) / size);
+    int32_t lo, hi;
+    f8_rows_of(a, e0, lane, &most, &lo, &hi);
+    const int32_t tiles = (hi - lo + size - 1) / size;
     const int32_t upto = lanes_up_to(tiles, lane);
     const uint64_t behind = __ballot(before + upto > tile);
     if (behind) {
@@ -58,9 +76,7 @@ __device__ __forceinline__ F8Rows f8_group_tile(const F8DotArgs& a, int64_t tile
       const int64_t row = lo + (tile - before - (upto - tiles)) * size;
       F8Rows r;
       r.first = __builtin_amdgcn_readlane(int32_t(row), first);
-      r.end = __builtin_amdgcn_readlane(int32_t(hi), first);
-      // (offsets that go down could give a number of tiles that has overflowed)
-      if (r.first < __builtin_amdgcn_readlane(int32_t(lo), first)) r.end = r.first;
+      r.end = __builtin_amdgcn_readlane(hi, first);
       r.expert = e0 + first;
       return r;
     }

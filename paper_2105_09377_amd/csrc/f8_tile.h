@@ -103,13 +103,10 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
   F8Rows rows = {0, a.M, 0};
   int part = 0;
   if constexpr (GROUPED) {
-    // (whatever the offsets are: no more tiles than there are workgroups for)
-    const int64_t there = f8_group_tiles(a, BM);
-    tiles_m = there < 0 ? 0 : there < tiles_m ? uint32_t(there) : tiles_m;
+    tiles_m = uint32_t(f8_group_tiles(a, BM));
     if (blockIdx.x >= tiles_m * tiles_n) return;
     mx4_tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
     rows = f8_group_tile(a, tm, BM);
-    if (rows.end <= rows.first) return;
   } else {
     const uint32_t tiles = tiles_m * tiles_n;
     part = int(blockIdx.x / tiles);
