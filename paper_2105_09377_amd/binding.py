@@ -636,7 +636,8 @@ def expert_sort(experts: torch.Tensor, n_experts: int, out: Optional[ExpertSort]
 
 
 def expert_split(x: torch.Tensor, places: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Tokens x (tokens, ..) -> rows, every token at the places of its choices; rows that are nobody's stay as they were."""
+    """Tokens x (tokens, ..) -> rows, every token at the places of its choices; rows that are nobody's are zeros, and stay as they were in
+    `out` (which saves filling a new tensor first)."""
     return _m().expert_split(x, places, out)
 
 
@@ -650,13 +651,13 @@ def expert_join(rows: torch.Tensor, places: torch.Tensor, weights: Optional[torc
 def expert_join_grad(grad: torch.Tensor, rows: torch.Tensor, places: torch.Tensor, weights: Optional[torch.Tensor] = None,
                      grad_rows: Optional[torch.Tensor] = None,
                      grad_weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """The gradients of `expert_join`'s rows and weights, of the gradient of its result; gradients of rows that are nobody's stay as they
-    were."""
+    """The gradients of `expert_join`'s rows and weights, of the gradient of its result; gradients of rows that are nobody's are zeros, and
+    stay as they were in `grad_rows` (which saves filling a new tensor first)."""
     return _m().expert_join_grad(grad, rows, places, weights, grad_rows, grad_weights)
 
 
 def f8_expert_dot(a0: F8, w: F8, offsets: torch.Tensor, tokens: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
                   act: int = GS_ACT_NONE, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Row r -> a0's row tokens[r] (r without tokens) times the matrix of w ((experts, n), (k)) whose expert has row r by `offsets`;
-    rows of no expert stay as they were."""
+    rows of no expert are zeros, and stay as they were in `out` (which saves filling a new tensor first)."""
     return _m().f8_expert_dot(a0, w, offsets, tokens, out_dtype, act, out, workspace)

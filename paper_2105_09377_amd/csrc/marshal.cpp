@@ -229,7 +229,8 @@ void call(const char* where, F&& f) {
 struct Result {
   PyObject* object;      // a new reference
   at::Tensor value;
-  Result(PyObject* out, PyObject* dtype, at::ScalarType otherwise, const int64_t* shape, int rank, const at::Tensor& like) {
+  // cleared: a new tensor is zeros, of which a call writes a part.
+  Result(PyObject* out, PyObject* dtype, at::ScalarType otherwise, const int64_t* shape, int rank, const at::Tensor& like, bool cleared = false) {
     if (out != Py_None) {
       value = tensor(out);
       object = out;
@@ -245,6 +246,7 @@ struct Result {
       st = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
     }
     value = at::empty(at::IntArrayRef(shape, rank), at::TensorOptions().dtype(st).device(like.device()));
+    if (cleared) value.zero_();
     object = THPVariable_Wrap(value);
     if (!object) throw Failed{};
   }
@@ -945,7 +947,7 @@ PyObject* py_f8_expert_dot(PyObject*, PyObject* const* p, Py_ssize_t n) {
     if (tokens.defined()) shape[0] = tokens.size(0);
     else
       for (int i = 0; i < a0.d.n_access; ++i) shape[0] *= a0.d.shape[i];
-    Result out(p[6], p[4], at::kFloat, shape, 2, a0.values);
+    Result out(p[6], p[4], at::kFloat, shape, 2, a0.values, true);
     r = out.object;
     const gs_ap fa = describe(offsets, 1);
     gs_ap ta{}, oa = describe_all(out.value);
@@ -1009,7 +1011,7 @@ PyObject* py_expert_split(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded(n, 3, [&](PyObject*& r) {
     const at::Tensor &x = tensor(p[0]), &places = tensor(p[1]);
     const RowsShape shape(x, places.numel());
-    Result rows(p[2], Py_None, x.scalar_type(), shape.v, shape.rank, x);
+    Result rows(p[2], Py_None, x.scalar_type(), shape.v, shape.rank, x, true);
     r = rows.object;
     const gs_ap xa = describe(x, 1), pa = describe_all(places);
     gs_ap ra = describe(rows.value, 1);
@@ -1042,7 +1044,7 @@ PyObject* py_expert_join_grad(PyObject*, PyObject* const* p, Py_ssize_t n) {
     const at::Tensor &grad = tensor(p[0]), &rows = tensor(p[1]), &places = tensor(p[2]);
     const at::Tensor weights = optional_tensor(p[3]);
     const RowsShape shape(rows, rows.dim() ? rows.size(0) : 0);
-    const Result grad_rows(p[4], Py_None, rows.scalar_type(), shape.v, shape.rank, rows);
+    const Result grad_rows(p[4], Py_None, rows.scalar_type(), shape.v, shape.rank, rows, true);
     const Owned rows_held(grad_rows.object);
     const Result grad_weights(p[5], Py_None, at::kFloat, places.sizes().data(), int(places.dim()), rows);
     const Owned weights_held(grad_weights.object);

@@ -60,9 +60,12 @@ class Decoder8Stack:
             a = gs.f8_dot(gs.f8_quantize(a.view(batch * tokens, self.heads * self.head_dim)), w["o"], out_dtype=bf16)
             y, rows = gs.f8_norm(rows, w["norm_experts"], residual=a, eps=self.eps)
             experts, weights = self.route(i, y)
-            s = gs.expert_sort(experts, w["up"].shape[0])
-            h = gs.f8_expert_dot(y, w["up"], s.offsets, tokens=s.tokens, out_dtype=bf16, act=gs.GS_ACT_RELU)
-            h = gs.f8_expert_dot(gs.f8_quantize(h), w["down"], s.offsets, out_dtype=bf16)
+            n_experts, hidden = w["up"].shape[:2]
+            s = gs.expert_sort(experts, n_experts)
+            # (rows of dropped choices, which no call below looks at, need not be zeros as in new results)
+            up, down = (torch.empty(s.tokens.shape[0], n, dtype=bf16, device=x.device) for n in (hidden, width))
+            h = gs.f8_expert_dot(y, w["up"], s.offsets, tokens=s.tokens, act=gs.GS_ACT_RELU, out=up)
+            h = gs.f8_expert_dot(gs.f8_quantize(h), w["down"], s.offsets, out=down)
             added = gs.expert_join(h, s.places, weights)
         if added is not None:
             rows = gs.pair_reduce(rows, added)
