@@ -21,8 +21,8 @@
  *     and fixes no storage type).  bfloat16 stores round to nearest even.
  *   - A result never shares bytes with an input (nothing works in place).  The data-moving
  *     transformers, glenside_depthwise_conv2d, norms and _expert_sort, _split, _join and _join_grad
- *     check this of access patterns (partial overlap included) and return GS_ERR_UNSUPPORTED; for
- *     the other entry points it is the caller's duty.
+ *     check this (partial overlap included; of what they are given, not of workspaces) and return
+ *     GS_ERR_UNSUPPORTED; for the other entry points it is the caller's duty.
  *   - Extensions that the paper does not have are marked EXT: padding, ReLU, scaling, a fused
  *     residual input.  With pad = 0, act = GS_ACT_NONE, scale = 1 and residual = NULL every entry
  *     point computes exactly the paper's expression.

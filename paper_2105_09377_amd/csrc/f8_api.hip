@@ -27,6 +27,8 @@ struct Matrices {
   int64_t mats, rows, cols;
   int64_t count() const { return mats * rows; }
 };
+int64_t values_bytes(const Matrices& m) { return m.count() * f8_blocks(m.cols) * kF8Block; }
+int64_t scales_bytes(const Matrices& m, int block_rows) { return m.mats * ceil_div(m.rows, block_rows) * f8_scale_pitch(m.cols) * 4; }
 
 // `need_data` as for check_ap.
 int check_f8(const gs_f8* m, bool need_data, Matrices* of) {
@@ -70,6 +72,17 @@ bool shares(std::initializer_list<const gs_ap*> results, std::initializer_list<c
     for (const gs_ap* in : inputs)
       if (r && in && overlaps(r, in)) return true;
   return false;
+}
+
+// An array of a pattern held in F8, as bytes.
+gs_ap bytes_of(void* data, int64_t bytes) {
+  gs_ap a;
+  memset(&a, 0, sizeof(a));
+  a.data = data;
+  a.dtype = GS_I8;
+  a.rank = 1;
+  a.shape[0] = bytes;
+  return a;
 }
 
 bool is_float(int dtype) { return dtype == GS_BF16 || dtype == GS_F32; }
@@ -232,13 +245,13 @@ int rows_args(const gs_ap* flat, const gs_ap* rows, const gs_ap* places, const g
 
 extern "C" {
 
-int glenside_f8_sizes(const gs_f8* m, size_t* values_bytes, size_t* scales_bytes) {
+int glenside_f8_sizes(const gs_f8* m, size_t* values, size_t* scales) {
   Matrices of;
   const int st = check_f8(m, false, &of);
   if (st) return st;
-  if (!values_bytes || !scales_bytes) return GS_ERR_NULL;
-  *values_bytes = size_t(of.count() * f8_blocks(of.cols) * kF8Block);
-  *scales_bytes = size_t(of.mats * ceil_div(of.rows, m->block_rows) * f8_scale_pitch(of.cols) * 4);
+  if (!values || !scales) return GS_ERR_NULL;
+  *values = size_t(values_bytes(of));
+  *scales = size_t(scales_bytes(of, m->block_rows));
   return GS_OK;
 }
 
@@ -278,7 +291,9 @@ int glenside_f8_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight,
   if (st) return st;
   if (out->rank != x->rank || out->n_access != x->n_access) return GS_ERR_RANK;
   if (!same_pattern_shape(out, x)) return GS_ERR_SHAPE;
-  if (out->block_rows != 1 || shares({sum}, {x, residual, weight})) return GS_ERR_UNSUPPORTED;
+  if (out->block_rows != 1) return GS_ERR_UNSUPPORTED;
+  const gs_ap values = bytes_of(out->values, values_bytes(of)), scales = bytes_of(out->scales, scales_bytes(of, 1));
+  if (shares({sum, &values, &scales}, {x, residual, weight})) return GS_ERR_UNSUPPORTED;
   a.out = out->values;
   a.scales = static_cast<float*>(out->scales);
   a.out_dtype = GS_F8;
