@@ -19,7 +19,8 @@
  *   - Element types: GS_I8 and GS_BF16 inputs to contractions accumulate in int32 and fp32
  *     respectively (exact for integers, no saturation; the paper's own notation is real-valued
  *     and fixes no storage type).  bfloat16 stores round to nearest even.
- *   - A result never shares bytes with an input (nothing works in place).  The data-moving
+ *   - A result never shares bytes with an input (nothing works in place) or with another result of
+ *     the call (which norms and the calls on tokens check too).  The data-moving
  *     transformers, glenside_depthwise_conv2d, norms and _expert_sort, _split, _join and _join_grad
  *     check this (partial overlap included; of what they are given, not of workspaces) and return
  *     GS_ERR_UNSUPPORTED; for the other entry points it is the caller's duty.

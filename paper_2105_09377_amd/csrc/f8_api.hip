@@ -66,11 +66,15 @@ bool same_pattern_shape(const A* a, const B* b) {
   return true;
 }
 
-// Does any of the results share bytes with any of the inputs?  Each may be NULL.
+// Does any of the results share bytes with any of the inputs, or with another result?  Each may be NULL.
 bool shares(std::initializer_list<const gs_ap*> results, std::initializer_list<const gs_ap*> inputs) {
-  for (const gs_ap* r : results)
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (!*r) continue;
     for (const gs_ap* in : inputs)
-      if (r && in && overlaps(r, in)) return true;
+      if (in && overlaps(*r, in)) return true;
+    for (auto other = results.begin(); other != r; ++other)
+      if (*other && overlaps(*r, *other)) return true;
+  }
   return false;
 }
 
