@@ -191,7 +191,7 @@ constexpr TileWay kTileWays[] = {{kF8Tile32x64, 32, 64, 1.5, 0.29, 0.205, 0.0}, 
 // Up to 16 rows, 8 of every expert that has some on average, w goes through registers (128 x 4 rows of 64 experts, 2048 x 4096, 106 us that way and 109 in
 // 32x64 tiles; 256 x 4 154 and 108).  There two tiles of w to a workgroup, which then share x, where x has more than four rows and the chip
 // stays full (16 x 8192 x 8192 17.1 us against 21.0 with one; 1 x 8192 x 8192 16.1 and 14.0).
-// More rows: the tile, and how many workgroups share one's sum over K (eight slabs each at least), by the time that they should take: the slabs of the
+// More rows: the tile, and how many workgroups share one's sum over K (eight slabs each on average, five at least), by the time that they should take: the slabs of the
 // busiest compute unit and w read at 5.2 TB/s, the longer one and two fifths of the other; where sums are shared 3 us more for the second
 // launch, and the parts written and read, 8 bytes each at 4.5 TB/s.  Times that it chooses between, measured: 64 x 8192 x 8192 24.7 in 64x64 tiles, 19.8 by twos, 39 in 128x128; 256 x 8192 x 8192 32.8 in
 // 64x128, 39 in 64x64, 45 in 128x128; 512 x 8192 x 8192 46 in 128x128 with eight waves, 61 with four, 63 in 64x128; 1024 x 8192 x 8192 64 in 128x256, 68 in
