@@ -26,10 +26,6 @@ __device__ __forceinline__ int32_t f8_encode4(const float* x, float factor) {
   w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * factor, x[3] * factor, w, true);
   return factor == factor ? w : 0;
 }
-__device__ __forceinline__ i32x2 f8_encode8(const float (&x)[8], float scale) {
-  const float f = 1.0f / scale;
-  return i32x2{f8_encode4(x, f), f8_encode4(x + 4, f)};
-}
 __device__ __forceinline__ void f8_decode4(int32_t w, float scale, float* x) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   x[0] = a[0] * scale;
@@ -102,7 +98,7 @@ struct F8DotArgs {        // out[m][n] = sum_b xs[m][b] ws[n / w_rows][b] sum_{k
   // experts: rows offsets[e] .. offsets[e + 1] - 1 of the result are of expert e's matrix; row r is of x's row tokens[r], or r
   const int32_t* offsets; // null: one matrix for all rows
   const int32_t* tokens;
-  int64_t experts, x_count, x_least;   // x_count: rows of x
+  int64_t experts, x_count;            // x_count: rows of x
   int32_t splits;         // set by the launcher: workgroups that share the sum over K of a tile
 };
 // How a product is done.

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) norm_kernel(Nor
         for (int i = 0; i < 8; ++i) h[i] = i < left ? h[i] : 0.0f;
       const float scale = f8_scale(f8_block_top(h));
       if (piece >= pieces) return;
-      static_cast<i32x2*>(a.out)[row * pieces + piece] = f8_encode8(h, scale);
+      static_cast<i32x2*>(a.out)[row * pieces + piece] = encode(h, scale);
       if (piece % 16 == 0) {
         const int64_t block = piece / 16, run = round_up(blocks, kF8ScaleRun);
         float* const to = a.scales + (row * run + block);

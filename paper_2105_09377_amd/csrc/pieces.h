@@ -19,16 +19,13 @@ __device__ __forceinline__ float load_plain(const void* p, int64_t i, std::integ
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
 
-// N numbers (8 or 4) of a row from element `at` on, zero beyond `left` of them.  STREAM: they are not read again soon.
-template <int DT, int N, bool STREAM = true>
+// N numbers (8 or 4) of a row from element `at` on, zero beyond `left` of them.
+template <int DT, int N>
 __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_t left, float (&x)[N]) {
   if (left >= N) {
     if constexpr (DT == GS_BF16) {
       static_assert(N == 8, "16 bytes");
-      const i32x4_any2* const src = reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at);
-      i32x4 v;
-      if constexpr (STREAM) v = __builtin_nontemporal_load(src);
-      else v = *src;
+      const i32x4 v = __builtin_nontemporal_load(reinterpret_cast<const i32x4_any2*>(static_cast<const uint16_t*>(row) + at));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[2 * i] = __uint_as_float(uint32_t(v[i]) << 16);
@@ -37,10 +34,7 @@ __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_
     } else {
 #pragma unroll
       for (int h = 0; h < N / 4; ++h) {
-        const f32x4_any* const src = reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h);
-        f32x4_any v;
-        if constexpr (STREAM) v = __builtin_nontemporal_load(src);
-        else v = *src;
+        const f32x4_any v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(static_cast<const float*>(row) + at + 4 * h));
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * h + i] = v[i];
       }
@@ -54,7 +48,7 @@ __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_
 typedef int32_t i32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef int32_t i32_any __attribute__((aligned(1)));
 
-// 16 bytes of a tensor from byte `at` on, zeros beyond `left` of them.  What ends a row is read with what is in front of it, which is then moved
+// 16 bytes of a tensor from byte `at` on, zeros beyond `left` of them.  STREAM: they are not read again soon.  What ends a row is read with what is in front of it, which is then moved
 // out: one access, as for the others, where bytes one by one would have the wave wait for one lane's (rows of 2050 bfloat16 numbers joined in 66 us
 // that way, 55 this one).
 template <bool STREAM>
