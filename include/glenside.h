@@ -92,8 +92,10 @@ int glenside_access_windows(const gs_ap* in, const int64_t* window, const int64_
  * rewrite (Sec. 5.2).  a0 ((m..),(k..)), a1 ((n..),(k..)) with equal compute shapes ->
  * out ((m.., n..),()):  out[m, n] = sum_k a0[m, k] * a1[n, k].
  * Types: i8 x i8 -> i32;  bf16 x bf16 -> f32 or bf16 (fp32 accumulate);  EXT f8 x f8 -> f32 or
- * bf16 (fp32 accumulate; the matrix unit aligns the 64 products of a step to their largest
- * exponent before adding, absolute error up to about 3e-5 of sum_k |a0[m,k] a1[n,k]|).  EXT: act
+ * bf16 (fp32 accumulate; the matrix unit cuts eight products that it adds together to multiples
+ * of 2^-13 of the largest one's power of two: absolute error below 7 / 8192 of the sum, over all
+ * eights, of their largest products, 1e-5 of sum_k |a0[m,k] a1[n,k]| where magnitudes are alike,
+ * 4e-4 seen where they are spread over many powers of two).  EXT: act
  * applies ReLU to the result.  workspace is unused (pass NULL,
  * 0): no shape of this contraction splits its sum across workgroups.                            */
 int glenside_cartesian_dot(const gs_ap* a0, const gs_ap* a1, gs_ap* out, int act,
@@ -430,8 +432,8 @@ int glenside_f8_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight,
                      void* stream);
 
 /* compute dotProd (cartProd a0 a1) as glenside_cartesian_dot has it, on F8 operands of either kind of blocks: the 128
- * products of a block are added as there (absolute error up to about 3e-5 of the sum of their magnitudes), times the product of the two
- * scales, blocks one after the other, in fp32.  That product has to be finite (below 3.4e38; infinite, a block's results are
+ * products of a block are added as there (with that error), times the product of the two scales, blocks one after the other, in
+ * fp32.  That product has to be finite (below 3.4e38; infinite, a block's results are
  * infinite or NaN), and below 2^-126 loses bits.  out ((m.., n..),()) of bf16 or f32, act as there.  A compute shape without
  * elements gives zeros.  Patterns of several access dimensions in blocks of 128 rows: the last one has to be a multiple of
  * 128, or GS_ERR_UNSUPPORTED.  workspace: glenside_f8_dot_workspace bytes (may be 0; 16-byte aligned). */
