@@ -434,7 +434,8 @@ int glenside_f8_norm(const gs_ap* x, const gs_ap* residual, const gs_ap* weight,
 /* compute dotProd (cartProd a0 a1) as glenside_cartesian_dot has it, on F8 operands of either kind of blocks: the 128
  * products of a block are added as there (with that error), times the product of the two scales, blocks one after the other, in
  * fp32.  That product has to be finite (below 3.4e38; infinite, a block's results are
- * infinite or NaN), and below 2^-126 loses bits.  out ((m.., n..),()) of bf16 or f32, act as there.  A compute shape without
+ * infinite or NaN), and below 2^-126 loses bits.  out ((m.., n..),()) of bf16 or f32, act as there:
+ * ReLU makes a zero of NaN, as everywhere here, so that a block whose scale is NaN does not show behind it.  A compute shape without
  * elements gives zeros.  Patterns of several access dimensions in blocks of 128 rows: the last one has to be a multiple of
  * 128, or GS_ERR_UNSUPPORTED.  workspace: glenside_f8_dot_workspace bytes (may be 0; 16-byte aligned). */
 int glenside_f8_dot(const gs_f8* a0, const gs_f8* a1, gs_ap* out, int act, void* workspace, size_t workspace_bytes,

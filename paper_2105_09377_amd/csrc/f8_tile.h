@@ -8,8 +8,9 @@
 // x for each 16 rows; a wave's 128 rows of w or fewer have one scale where w is in blocks of 128 rows.  Scales come four slabs at a
 // time, 16 bytes of a row.
 //
-// 8192 cubed 439 us, 2.5 PFLOP/s, where the same without scales (gemm_nt_dma_kernel, which adds in the matrix unit) takes 423; 16384 rows of 16 experts with
-// 4096 x 4096 287, 1.9 PFLOP/s.  What bounds them: the table of tiles in f8_dot.hip.
+// 8192 cubed 433 to 449 us in a graph, 2.5 PFLOP/s (451 to 465 among others), where the same without scales (gemm_nt_dma_kernel, which adds in the matrix unit)
+// takes 423; 16384 rows of 16 experts with 4096 x 4096 287, 1.9 PFLOP/s, where they fill tiles, 309 to 318 drawn evenly.  What bounds them: the table
+// of tiles in f8_dot.hip.
 #pragma once
 
 #include "f8_group.h"
