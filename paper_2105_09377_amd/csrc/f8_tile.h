@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 2) f8_dot_tile_kernel(F8DotArg
     if (blockIdx.x >= tiles_m * tiles_n) return;
     mx4_tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
     rows = f8_group_tile(a, tm, BM);
+    if (rows.end <= rows.first) return;           // (only where offsets are written meanwhile, by a program's mistake)
   } else {
     const uint32_t tiles = tiles_m * tiles_n;
     part = int(blockIdx.x / tiles);

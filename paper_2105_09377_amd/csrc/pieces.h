@@ -48,9 +48,9 @@ __device__ __forceinline__ void load_numbers(const void* row, int64_t at, int64_
 typedef int32_t i32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef int32_t i32_any __attribute__((aligned(1)));
 
-// 16 bytes of a tensor from byte `at` on, zeros beyond `left` of them.  STREAM: they are not read again soon.  What ends a row is read with what is in front of it, which is then moved
-// out: one access, as for the others, where bytes one by one would have the wave wait for one lane's (rows of 2050 bfloat16 numbers joined in 66 us
-// that way, 55 this one).
+// 16 bytes of a tensor from byte `at` on, zeros beyond `left` of them.  STREAM: they are not read again soon.  What ends a row is read with what is in
+// front of it, which is then moved out: one access, as for the others, where bytes one by one would have the wave wait for one lane's (rows of 2050
+// bfloat16 numbers joined in 66 us that way, 55 this one).
 template <bool STREAM>
 __device__ __forceinline__ i32x4 load_16(const void* base, int64_t at, int64_t left) {
   const uint8_t* const p = static_cast<const uint8_t*>(base);
